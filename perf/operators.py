@@ -286,7 +286,7 @@ def run(state):
         if kind == "rope":
             ctx.locks_rope(s["rotary"], s["positions"], s["q"], s["q_out"], s["k_new"], s["k_out"])
         elif kind == "append":
-            ctx.locks_append(s["k_new"], s["v_new"], s["kv"], batch, rotary=s["rotary"], positions=s["positions"], q=s["q"],
+            ctx.locks_append_rows(s["k_new"], s["v_new"], s["kv"], batch, rotary=s["rotary"], positions=s["positions"], q=s["q"],
                              q_out=s["q_out"], cu_tokens=s["own_cu"])
         elif kind == "qappend":
             ctx.locks_kvq_append(s["k_new"], s["v_new"], s["kv"], batch, rotary=s["rotary"], positions=s["positions"], q=s["q"],
