@@ -350,6 +350,93 @@ int locks_profile_end(locks_ctx *ctx, float *stage_ms, int *steps);
  * synchronises `stream` and writes that replay's three stage durations (ms) to stage_ms[3]. */
 int locks_profile_read(locks_ctx *ctx, float *stage_ms, locks_stream stream);
 
+/* ---- Rotary positions, appends and an 8-bit cache -------------------------------------------------------------
+ * What surrounds the step in a serving engine.  locks_decode_step appends rows that are rotated already; these calls rotate
+ * queries and keys (positions with one axis for text, several for images and video), append whole batches of new tokens (a token
+ * per request, or chunks of prompts), and keep the cache in 8 bits.
+ *
+ * Rows: head h of token i at p + i * stride_token + h * stride_head (elements of kv_dtype = q_dtype), head_dim contiguous
+ * elements.  p 16-byte aligned, strides multiples of 16 bytes; slices of a fused projection's rows fit. */
+typedef struct {
+  void *p;
+  int64_t stride_token, stride_head;
+} locks_rows;
+
+/* Rotation: pair i < rot_dim / 2 of a head's dimensions turns by the angle position[axis[i]] * inv_freq[i] (formed in 64 bits, so
+ * that far positions keep theirs; rows in fp32, rounded once): (a, b) -> (a cos - b sin, a sin + b cos).  Pairs are
+ * (i, i + rot_dim / 2), or (2 i, 2 i + 1) if interleaved; dimensions from rot_dim on stay as they are.  A host struct, copied by
+ * the call.  rot_dim: a multiple of 16 up to head_dim; num_axes 1 .. 4; axis[i] < num_axes; inv_freq finite. */
+#define LOCKS_MAX_AXES 4
+typedef struct {
+  float inv_freq[64];
+  uint8_t axis[64];
+  int32_t rot_dim, num_axes, interleaved;
+} locks_rotary;
+
+/* Rotate num_tokens rows of q (Hq heads) and of k (Hkv heads); either pair may be NULL.  positions [num_axes][num_tokens] int32.
+ * An output may be its input (the same rows); otherwise the two must not overlap. */
+int locks_rope(locks_ctx *ctx, const locks_rotary *rot, const int32_t *positions, int num_tokens, const locks_rows *q,
+               const locks_rows *q_out, const locks_rows *k, const locks_rows *k_out, locks_stream stream);
+
+/* Append the keys and values of new tokens to the cache, rotating the keys, and the queries on the way.
+ *   cu_tokens   [batch + 1] int32: request b's new tokens are rows cu_tokens[b] .. cu_tokens[b+1] - 1 (none, if the two are equal);
+ *               rows behind the last request's belong to nobody, are not written and influence nothing.  NULL: one token per
+ *               request, num_tokens == batch; a request of length zero has none.
+ *   kv          seq_lens[b] = T_b counts the new tokens ALREADY (as for locks_select and locks_sparse_attend, and unlike
+ *               locks_decode_step; the layers of a model share the lengths): they take the places T_b - n_b .. T_b - 1.
+ *               Lengths are not changed.
+ *   positions   [num_axes][num_tokens] int32, or NULL: a token's place in its sequence, on every axis.
+ *   rot         NULL: rows are stored as they are; q and q_out are NULL then.
+ *   q, q_out    both or neither; q_out may be q.
+ * A request with more new tokens than T_b, a place beyond the block-table row or a block outside the cache: LOCKS_ERR_BAD_BLOCK in
+ * the status word, and nothing is written to the cache there. */
+int locks_append_rows(locks_ctx *ctx, const locks_rotary *rot, const int32_t *positions, const int32_t *cu_tokens, int num_tokens,
+                 const locks_rows *q, const locks_rows *q_out, const locks_rows *k_new, const locks_rows *v_new,
+                 const locks_kv *kv, int batch, locks_stream stream);
+
+/* Paged cache in 8 bits: a page's keys (and its values) of one KV head share one scale, value = code * scale.
+ *   LOCKS_KVQ_INT    signed integers: scale = max |x| / 127, code = x / scale rounded to even
+ *   LOCKS_KVQ_FLOAT  four exponent and three fraction bits (e4m3): scale = max |x| / 448, code = x / scale rounded to even
+ * A page whose largest magnitude is below 2^-100 is stored as zeros with a scale of zero; one with an infinity or a NaN gets a
+ * scale of NaN and codes of zero: whatever attends it is NaN.  Scales are fp32.
+ * Only complete pages are in codes.  The unfinished last page of the request in row b of the batch is kept as it comes, in fp32, in
+ * k_tail / v_tail [max_batch][Hkv][page_size][head_dim], and is quantised once, when its last token comes; so the codes do not
+ * depend on how a sequence was cut into appends.  A request that moves to another row takes its tail along; a block may
+ * be shared as in any paged cache. */
+#define LOCKS_KVQ_INT 0
+#define LOCKS_KVQ_FLOAT 1
+typedef struct {
+  void *k, *v;                                      /* codes; strides in elements (bytes), multiples of 16; bases 16-byte aligned */
+  int64_t stride_block, stride_head, stride_token;
+  int32_t num_blocks, fmt;                          /* LOCKS_KVQ_* */
+  float *k_scale, *v_scale;                         /* [num_blocks][Hkv] */
+  float *k_tail, *v_tail;                           /* 16-byte aligned */
+  const int32_t *block_table;                       /* [max_batch][max_pages_per_seq] */
+  const int32_t *seq_lens;                          /* [max_batch] */
+} locks_kvq;
+
+/* locks_append_rows for the 8-bit cache.  bf16 configurations (else UNSUPPORTED), pages of 16, 32 and 64 tokens.  cu_tokens has to
+ * ascend; a request whose rows do not lie in 0 .. num_tokens is reported (LOCKS_ERR_BAD_BLOCK) and left out. */
+int locks_kvq_append(locks_ctx *ctx, const locks_rotary *rot, const int32_t *positions, const int32_t *cu_tokens, int num_tokens,
+                     const locks_rows *q, const locks_rows *q_out, const locks_rows *k_new, const locks_rows *v_new,
+                     const locks_kvq *kv, int batch, locks_stream stream);
+
+/* Attention over the 8-bit cache: for every row of q, softmax(q.k_i sm_scale)-weighted mean of v_i.  bf16 configurations.
+ *   q            [num_tokens][Hq][d], out likewise, lse optional [num_tokens][Hq] fp32 (natural log)
+ *   cu_tokens    NULL: one token per request (num_tokens == batch), which sees its T_b tokens; else as in locks_append_rows, and
+ *                token j of request b sees the first T_b - n_b + j + 1 tokens (drafted tokens, a chunk of a prompt)
+ *   page_ids     [batch][Hkv][k] and page_count [batch][Hkv], as locks_select writes them (LOCKS_COMBINE_PER_HEAD: one table per
+ *                query head), or both NULL: every page.  One token per request only (with cu_tokens: INVALID_ARG).
+ * A row that sees nothing gets zeros and a lse of -inf.  Rows behind the last request's are left as they were.  Lengths, counts, page
+ * and block ids out of range are reported (LOCKS_ERR_BAD_BLOCK) and skipped. */
+int locks_kvq_attend(locks_ctx *ctx, const void *q, const int32_t *cu_tokens, int num_tokens, const locks_kvq *kv, int batch,
+                     const int32_t *page_ids, const int32_t *page_count, void *out, float *lse, locks_stream stream);
+
+/* locks_build_summaries from the codes: the summaries of complete pages of the 8-bit cache, which locks_select then scores
+ * (locks_select and locks_scan read block_table and seq_lens of their locks_kv only).  bf16 configurations. */
+int locks_kvq_build_summaries(locks_ctx *ctx, const locks_kvq *kv, int batch, const int32_t *page_begin, const int32_t *page_end,
+                              void *summaries, locks_stream stream);
+
 /* locks_sparse_attend for callers that cannot allocate device memory (the paper has no
  * counterpart; this is a convenience of the library).  Some hosts of this code may not call
  * cudaMalloc at all: a plugin running inside an engine that has already handed the whole device to

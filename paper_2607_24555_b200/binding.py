@@ -21,7 +21,8 @@ SYMBOLS = ["locks_summary_bytes", "locks_workspace_bytes", "locks_create", "lock
            "locks_host_cache_clear", "locks_select_exact", "locks_selection_quality",
            "locks_select_rival", "locks_fake_quantize_pages", "locks_scan",
            "locks_select_scored", "locks_merge_selection", "locks_merge_attention",
-           "locks_build_summaries_layers"]
+           "locks_build_summaries_layers", "locks_rope", "locks_append_rows", "locks_kvq_append", "locks_kvq_attend",
+           "locks_kvq_build_summaries"]
 
 
 PARTITION_AUTO, PARTITION_STRIDED, PARTITION_BALANCED = 0, 1, 2   # LOCKS_PARTITION_* of include/locks.h
@@ -44,6 +45,25 @@ class KV(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("stride_block", C.c_int64), ("stride_head", C.c_int64),
                 ("stride_token", C.c_int64), ("num_blocks", C.c_int32), ("block_table", C.c_void_p),
                 ("seq_lens", C.c_void_p)]
+
+
+KVQ_INT, KVQ_FLOAT = 0, 1   # LOCKS_KVQ_*
+
+
+class KVQ(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("stride_block", C.c_int64), ("stride_head", C.c_int64),
+                ("stride_token", C.c_int64), ("num_blocks", C.c_int32), ("fmt", C.c_int32), ("k_scale", C.c_void_p),
+                ("v_scale", C.c_void_p), ("k_tail", C.c_void_p), ("v_tail", C.c_void_p), ("block_table", C.c_void_p),
+                ("seq_lens", C.c_void_p)]
+
+
+class Rows(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("stride_token", C.c_int64), ("stride_head", C.c_int64)]
+
+
+class Rotary(C.Structure):
+    _fields_ = [("inv_freq", C.c_float * 64), ("axis", C.c_uint8 * 64), ("rot_dim", C.c_int32), ("num_axes", C.c_int32),
+                ("interleaved", C.c_int32)]
 
 
 _lib = None
@@ -107,6 +127,14 @@ def lib():
         L.locks_select_exact.restype = C.c_int
         L.locks_selection_quality.argtypes = [vp, vp, C.POINTER(KV), C.c_int, i32p, i32p, i32p, i32p, i32p, C.c_int, vp, vp]
         L.locks_selection_quality.restype = C.c_int
+        rows, rotary, kvq = C.POINTER(Rows), C.POINTER(Rotary), C.POINTER(KVQ)
+        L.locks_rope.argtypes = [vp, rotary, vp, C.c_int, rows, rows, rows, rows, vp]
+        L.locks_append_rows.argtypes = [vp, rotary, vp, vp, C.c_int, rows, rows, rows, rows, C.POINTER(KV), C.c_int, vp]
+        L.locks_kvq_append.argtypes = [vp, rotary, vp, vp, C.c_int, rows, rows, rows, rows, kvq, C.c_int, vp]
+        L.locks_kvq_attend.argtypes = [vp, vp, vp, C.c_int, kvq, C.c_int, vp, vp, vp, vp, vp]
+        L.locks_kvq_build_summaries.argtypes = [vp, kvq, C.c_int, vp, vp, vp, vp]
+        for fn in ("locks_rope", "locks_append_rows", "locks_kvq_append", "locks_kvq_attend", "locks_kvq_build_summaries"):
+            getattr(L, fn).restype = C.c_int
         L.locks_strerror.restype = C.c_char_p
         L.locks_strerror.argtypes = [C.c_int]
         for fn in ("locks_create", "locks_destroy", "locks_build_summaries", "locks_select", "locks_sparse_attend",
@@ -161,6 +189,82 @@ def make_config(Hq, Hkv, rank, fmt, dtype, max_batch, max_pages, budget, sm_scal
     return Config(d, B, Hq, Hkv, rank, f, dt, dt, max_batch, max_pages, budget, sm_scale, combine)
 
 
+def make_rotary(inv_freq, axis=None, interleaved=False) -> Rotary:
+    """Rotary description (locks_rotary): frequency and position axis of each rotated pair of a head's dimensions.
+
+    inv_freq: rot_dim / 2 numbers; axis: as many axis indexes (None: one axis)."""
+    n = len(inv_freq)
+    if not 0 < n <= 64 or (axis is not None and len(axis) != n):
+        raise LocksError("make_rotary: at most 64 frequencies, and an axis for each")
+    r = Rotary()
+    for i in range(n):
+        r.inv_freq[i] = float(inv_freq[i])
+        a = 0 if axis is None else int(axis[i])
+        if not 0 <= a < 4:
+            raise LocksError("make_rotary: axes are 0 .. 3")
+        r.axis[i] = a
+    r.rot_dim, r.num_axes, r.interleaved = 2 * n, 1 if axis is None else max(int(a) for a in axis) + 1, int(bool(interleaved))
+    return r
+
+
+def _need(ok, what):
+    if not ok:
+        raise LocksError(what)
+
+
+@dataclass
+class KVQView:
+    """A paged cache in 8 bits.  k, v: [block, head, token, dim] int8 or float8_e4m3fn tensors (views of any layout whose dims are
+    contiguous); k_scale, v_scale: [block, head] fp32; k_tail, v_tail: [max_batch, head, page_size, dim] fp32."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+    k_tail: torch.Tensor
+    v_tail: torch.Tensor
+    block_table: torch.Tensor   # [max_batch, max_pages] int32, device
+    seq_lens: torch.Tensor      # [max_batch] int32, device
+
+    def __post_init__(self):
+        k, v, f32, i32 = self.k, self.v, torch.float32, torch.int32
+        _need(k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and k.stride(3) == 1, "KVQView: k and v are [block, head, token, dim], dims contiguous, laid out alike")
+        _need(k.dtype == v.dtype and k.dtype in (torch.int8, torch.float8_e4m3fn), "KVQView: codes are int8 or float8_e4m3fn")
+        for t in (self.k_scale, self.v_scale):
+            _need(t.dtype == f32 and t.shape == k.shape[:2] and t.is_contiguous(), "KVQView: scales are contiguous fp32 [block, head]")
+        for t in (self.k_tail, self.v_tail):
+            _need(t.dtype == f32 and t.dim() == 4 and t.shape[1:] == k.shape[1:] and t.is_contiguous(), "KVQView: tails are contiguous fp32 [max_batch, head, page_size, dim]")
+        _need(self.block_table.dtype == i32 and self.block_table.dim() == 2 and self.block_table.is_contiguous(), "KVQView: block_table is contiguous int32 [max_batch, max_pages]")
+        _need(self.seq_lens.dtype == i32 and self.seq_lens.dim() == 1 and self.seq_lens.is_contiguous(), "KVQView: seq_lens is contiguous int32 [max_batch]")
+        _need(all(t.device == k.device for t in (v, self.k_scale, self.v_scale, self.k_tail, self.v_tail, self.block_table, self.seq_lens)), "KVQView: tensors on different devices")
+
+    def struct(self) -> KVQ:
+        sb, sh, st, _ = self.k.stride()
+        return KVQ(self.k.data_ptr(), self.v.data_ptr(), sb, sh, st, self.k.shape[0], KVQ_INT if self.k.dtype == torch.int8 else KVQ_FLOAT,
+                   self.k_scale.data_ptr(), self.v_scale.data_ptr(), self.k_tail.data_ptr(), self.v_tail.data_ptr(),
+                   self.block_table.data_ptr(), self.seq_lens.data_ptr())
+
+    def kv_view(self) -> "KVView":
+        """For locks_select and locks_scan, which read the block table and the lengths only."""
+        return KVView(self.k, self.v, self.k.stride()[:3], self.k.shape[0], self.block_table, self.seq_lens)
+
+
+def new_kvq_cache(num_blocks, max_batch, Hkv, page_size, block_table, seq_lens, fmt="int8", layout="HND") -> KVQView:
+    """An empty 8-bit cache on the table's device; layout "HND" [block, head, token, dim] or "NHD" [block, token, head, dim] in memory."""
+    dev, d = block_table.device, 128
+    dt = {"int8": torch.int8, "e4m3": torch.float8_e4m3fn}[fmt]
+
+    def codes():
+        if layout == "NHD":
+            return torch.zeros(num_blocks, page_size, Hkv, d, dtype=torch.uint8, device=dev).view(dt).transpose(1, 2)
+        return torch.zeros(num_blocks, Hkv, page_size, d, dtype=torch.uint8, device=dev).view(dt)
+
+    def f32(*shape):
+        return torch.zeros(*shape, dtype=torch.float32, device=dev)
+
+    return KVQView(codes(), codes(), f32(num_blocks, Hkv), f32(num_blocks, Hkv), f32(max_batch, Hkv, page_size, d),
+                   f32(max_batch, Hkv, page_size, d), block_table, seq_lens)
+
+
 @dataclass
 class KVView:
     """A paged cache: torch tensors plus element strides (block, head, token)."""
@@ -177,12 +281,32 @@ class KVView:
                   self.seq_lens.data_ptr())
 
 
+class _Device:
+    """Makes a device current for a call, if it is not (a context's workspace and attributes belong to its device)."""
+    __slots__ = ("index", "was")
+
+    def __init__(self, device):
+        self.index = device.index
+
+    def __enter__(self):
+        self.was = torch.cuda.current_device()
+        if self.was != self.index:
+            torch.cuda.set_device(self.index)
+
+    def __exit__(self, *exc):
+        if self.was != self.index:
+            torch.cuda.set_device(self.was)
+
+
 class Context:
     """Owns a locks_ctx and its torch-allocated workspace.  Methods mirror the C entry points."""
 
     def __init__(self, cfg: Config, device="cuda:0"):
         self.cfg = cfg
         self.device = torch.device(device)
+        if self.device.type == "cuda" and self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self._dtype = torch.bfloat16 if cfg.q_dtype == BF16 else torch.float32
         L = lib()
         nbytes = locks_workspace_bytes(cfg)
         if nbytes == 0:
@@ -300,6 +424,112 @@ class Context:
         _check(lib().locks_decode_step_host(self.handle, _ptr(q_host), _ptr(k_new_host), _ptr(v_new_host), C.byref(s),
                                             _ptr(summaries), batch, _ptr(out_host), _ptr(page_ids_host),
                                             _ptr(page_count_host), _stream(stream)), "locks_decode_step_host")
+
+    # ---- rotary positions, appends and the 8-bit cache.  Tensors are checked here: type, shape, strides, device.
+    def _rows(self, t, heads, n, what):
+        _need(t.dim() == 3 and t.shape[0] == n and t.shape[1] == heads and t.shape[2] == 128 and t.stride(2) == 1,
+              f"{what}: [tokens, {heads}, 128] with contiguous dims expected, got {tuple(t.shape)}")
+        _need(t.dtype == self._dtype and t.device == self.device, f"{what}: {self._dtype} on {self.device} expected")
+        return C.byref(Rows(t.data_ptr(), t.stride(0), t.stride(1)))
+
+    def _ints(self, t, shape, what):
+        if t is None:
+            return None
+        _need(t.dtype == torch.int32 and tuple(t.shape) == shape and t.is_contiguous() and t.device == self.device,
+              f"{what}: contiguous int32 {shape} on {self.device} expected")
+        return t.data_ptr()
+
+    def _launch(self, stream):
+        """The stream to launch on, of this context's device."""
+        if stream is None:
+            return torch.cuda.current_stream(self.device).cuda_stream
+        return stream if isinstance(stream, int) else stream.cuda_stream
+
+    def _positions(self, rotary, positions, n):
+        if positions is None:
+            return None
+        if positions.dim() == 1:
+            positions = positions[None]
+        return self._ints(positions, (rotary.num_axes, n), "positions")
+
+    def _view_ok(self, view, batch, what):
+        c = self.cfg
+        _need(view.k.device == self.device, f"{what}: a cache on {self.device} expected")
+        _need(1 <= batch <= c.max_batch and view.seq_lens.shape[0] >= batch and view.block_table.shape[0] >= batch and
+              view.block_table.shape[1] == c.max_pages_per_seq, f"{what}: batch, lengths or block table do not fit the configuration")
+
+    def _kvq_ok(self, kvq, batch, what):
+        self._view_ok(kvq, batch, what)
+        _need(tuple(kvq.k.shape[1:]) == (self.cfg.num_kv_heads, self.cfg.page_size, 128) and kvq.k_tail.shape[0] >= batch,
+              f"{what}: the cache's heads, page size or tails do not fit the configuration")
+
+    def locks_rope(self, rotary, positions, q, q_out, k=None, k_out=None, stream=None):
+        """Rotate q [tokens, Hq, 128] into q_out and k [tokens, Hkv, 128] into k_out (either pair may be None; in place: pass a
+        tensor twice).  positions: int32 [axes, tokens], or [tokens] with one axis."""
+        c, L = self.cfg, lib()
+        _need(rotary is not None and positions is not None, "locks_rope: rotary and positions are needed")
+        _need((q is None) == (q_out is None) and (k is None) == (k_out is None) and (q is not None or k is not None), "locks_rope: q with q_out, k with k_out")
+        n = (q if q is not None else k).shape[0]
+        r = [None if t is None else self._rows(t, h, n, "locks_rope") for t, h in
+             ((q, c.num_q_heads), (q_out, c.num_q_heads), (k, c.num_kv_heads), (k_out, c.num_kv_heads))]
+        with _Device(self.device):
+            _check(L.locks_rope(self.handle, C.byref(rotary), self._positions(rotary, positions, n), n, *r, self._launch(stream)), "locks_rope")
+
+    def _append(self, fn, what, kv, k_new, v_new, batch, rotary, positions, q, q_out, cu_tokens, stream):
+        c, n = self.cfg, k_new.shape[0]
+        _need(rotary is not None or (q is None and q_out is None and positions is None), f"{what}: q and positions go with a rotary description")
+        _need((q is None) == (q_out is None), f"{what}: q with q_out")
+        r = [None if t is None else self._rows(t, h, n, what) for t, h in
+             ((q, c.num_q_heads), (q_out, c.num_q_heads), (k_new, c.num_kv_heads), (v_new, c.num_kv_heads))]
+        cu = self._ints(cu_tokens, (batch + 1,), f"{what}: cu_tokens")
+        pos = None if positions is None else self._positions(rotary, positions, n)
+        s = kv.struct()
+        with _Device(self.device):
+            _check(fn(self.handle, None if rotary is None else C.byref(rotary), pos, cu, n, *r, C.byref(s), batch, self._launch(stream)), what)
+
+    def locks_append_rows(self, k_new, v_new, kv: KVView, batch, rotary=None, positions=None, q=None, q_out=None, cu_tokens=None,
+                          stream=None):
+        """Append k_new, v_new [tokens, Hkv, 128] (keys rotated, if there is a rotary description) to the cache and rotate q into
+        q_out.  kv.seq_lens counts the new tokens already; cu_tokens: see include/locks.h."""
+        self._view_ok(kv, batch, "locks_append_rows")
+        _need(kv.k.dtype == kv.v.dtype == self._dtype and kv.v.device == self.device, f"locks_append_rows: a {self._dtype} cache on {self.device} expected")
+        self._append(lib().locks_append_rows, "locks_append_rows", kv, k_new, v_new, batch, rotary, positions, q, q_out, cu_tokens, stream)
+
+    def locks_kvq_append(self, k_new, v_new, kvq: KVQView, batch, rotary=None, positions=None, q=None, q_out=None, cu_tokens=None,
+                         stream=None):
+        """locks_append_rows for the 8-bit cache: complete pages as codes, the unfinished one in the tails."""
+        self._kvq_ok(kvq, batch, "locks_kvq_append")
+        self._append(lib().locks_kvq_append, "locks_kvq_append", kvq, k_new, v_new, batch, rotary, positions, q, q_out, cu_tokens, stream)
+
+    def locks_kvq_attend(self, q, kvq: KVQView, batch, out, lse=None, page_ids=None, page_count=None, cu_tokens=None, stream=None):
+        """Attention of q [tokens, Hq, 128] over the 8-bit cache into out; one token per request (all pages, or page_ids and
+        page_count of locks_select), or with cu_tokens several, each seeing what is before it."""
+        c, n = self.cfg, q.shape[0]
+        self._kvq_ok(kvq, batch, "locks_kvq_attend")
+        for t in (q, out):
+            _need(t.shape == (n, c.num_q_heads, 128) and t.is_contiguous() and t.dtype == self._dtype and t.device == self.device,
+                  f"locks_kvq_attend: q and out are contiguous {self._dtype} [tokens, {c.num_q_heads}, 128] on {self.device}")
+        _need(lse is None or (lse.shape == (n, c.num_q_heads) and lse.is_contiguous() and lse.dtype == torch.float32 and lse.device == self.device),
+              "locks_kvq_attend: lse is contiguous fp32 [tokens, Hq]")
+        heads = c.num_q_heads if c.combine == COMBINE_PER_HEAD else c.num_kv_heads
+        ids = self._ints(page_ids, (batch, heads, self.k), "locks_kvq_attend: page_ids")
+        cnt = self._ints(page_count, (batch, heads), "locks_kvq_attend: page_count")
+        cu = self._ints(cu_tokens, (batch + 1,), "locks_kvq_attend: cu_tokens")
+        s = kvq.struct()
+        with _Device(self.device):
+            _check(lib().locks_kvq_attend(self.handle, q.data_ptr(), cu, n, C.byref(s), batch, ids, cnt, out.data_ptr(),
+                                          None if lse is None else lse.data_ptr(), self._launch(stream)), "locks_kvq_attend")
+
+    def locks_kvq_build_summaries(self, kvq: KVQView, batch, summaries, page_begin=None, page_end=None, stream=None):
+        """locks_build_summaries from the codes of the 8-bit cache."""
+        self._kvq_ok(kvq, batch, "locks_kvq_build_summaries")
+        _need(summaries.dtype == torch.uint8 and summaries.is_contiguous() and summaries.device == self.device and
+              summaries.numel() >= kvq.k.shape[0] * self.cfg.num_kv_heads * self.summary_bytes, "locks_kvq_build_summaries: summaries of Context.new_summaries expected")
+        s = kvq.struct()
+        with _Device(self.device):
+            _check(lib().locks_kvq_build_summaries(self.handle, C.byref(s), batch, self._ints(page_begin, (batch,), "page_begin"),
+                                                   self._ints(page_end, (batch,), "page_end"), summaries.data_ptr(), self._launch(stream)),
+                   "locks_kvq_build_summaries")
 
     def locks_poll_status(self, stream=None) -> int:
         st = C.c_int32(0)

@@ -2,7 +2,7 @@
 #include <mutex>
 #include <new>
 
-#include "locks_internal.cuh"
+#include "kvq.cuh"
 
 namespace {
 
@@ -35,7 +35,7 @@ int validate(const locks_config *c) {
 }
 
 struct Layout {
-  size_t status, shat, part, part_cnt, sel_done, cand_val, cand_idx, att_o, att_lse, att_done, ids, cnt, sq, skn, svn, sout, seq_eff, arrivals, stage_summ, total;
+  size_t status, shat, part, part_cnt, sel_done, cand_val, cand_idx, att_o, att_lse, att_done, ids, cnt, sq, skn, svn, sout, seq_eff, arrivals, stage_summ, kvq_part, kvq_ml, kvq_done, total;
   int G, k, S, max_groups, sel_ept, sel_chunks, sel_kc;
 };
 
@@ -105,6 +105,10 @@ Layout make_layout(const locks_config *c) {
   L.seq_eff = take(2 * nb * 4);
   L.arrivals = take(nb * (1 + Hkv) * 4);
   L.stage_summ = take(nb * Hkv * L.S);
+  const bool kvq = c->kv_dtype == LOCKS_BF16;   // (the 8-bit cache goes with bf16 queries)
+  L.kvq_part = take(kvq ? kvq_part_floats() * 4 : 0);
+  L.kvq_ml = take(kvq ? kvq_ml_floats() * 4 : 0);
+  L.kvq_done = take(KVQ_SLOT_BOUND * 4);
   L.total = o;
   return L;
 }
@@ -207,6 +211,9 @@ int locks_create(const locks_config *cfg, void *workspace, size_t ws_bytes, lock
   c->arrivals = reinterpret_cast<int32_t *>(ws + L.arrivals);
   c->staged = c->arrivals + cfg->max_batch;
   c->stage_summ = ws + L.stage_summ;
+  c->kvq_part = reinterpret_cast<float *>(ws + L.kvq_part);
+  c->kvq_ml = reinterpret_cast<float2 *>(ws + L.kvq_ml);
+  c->kvq_done = reinterpret_cast<int32_t *>(ws + L.kvq_done);
   c->stage_q = ws + L.sq; c->stage_kn = ws + L.skn; c->stage_vn = ws + L.svn; c->stage_out = ws + L.sout;
   if (cudaStreamCreateWithFlags(&c->side, cudaStreamNonBlocking) != cudaSuccess ||
       cudaEventCreateWithFlags(&c->ev_fork, cudaEventDisableTiming) != cudaSuccess ||
@@ -216,6 +223,7 @@ int locks_create(const locks_config *cfg, void *workspace, size_t ws_bytes, lock
       cudaMemsetAsync(c->sel_done, 0, (size_t)cfg->max_batch * cfg->num_q_heads * 4, 0) != cudaSuccess ||
       cudaMemsetAsync(c->part_cnt, 0, (size_t)cfg->max_batch * cfg->num_kv_heads * 4, 0) != cudaSuccess ||
       cudaMemsetAsync(c->arrivals, 0, (size_t)cfg->max_batch * (1 + cfg->num_kv_heads) * 4, 0) != cudaSuccess ||
+      cudaMemsetAsync(c->kvq_done, 0, KVQ_SLOT_BOUND * 4, 0) != cudaSuccess ||
       cudaStreamSynchronize(0) != cudaSuccess) {
     if (c->hint_host) cudaFreeHost(c->hint_host);
     delete c;

@@ -619,10 +619,14 @@ __global__ void __launch_bounds__(kBuildWarps * 32, kBuildCtasPerSm) build_kerne
   auto load_item = [&](int s, float (&v)[LOCKS_B][4]) {
     const int block = __shfl_sync(0xffffffffu, it_block, s);
     const T *K = reinterpret_cast<const T *>(kbase) + ((int64_t)block * p.sb + (int64_t)h * p.sh) + 4 * lane;
+    float scale = 1.f;
+    if constexpr (sizeof(T) == 1) scale = p.k_scale[(int64_t)block * p.Hkv + h];
 #pragma unroll
     for (int i = 0; i < LOCKS_B; ++i) {
       const T *src = K + (int64_t)i * p.st;
-      if (sizeof(T) == 2) {
+      if constexpr (sizeof(T) == 1) {
+        load_codes(src, scale, p.kvq_fmt, v[i]);
+      } else if (sizeof(T) == 2) {
         const uint2 w = *reinterpret_cast<const uint2 *>(src);
         v[i][0] = __uint_as_float(w.x << 16); v[i][1] = __uint_as_float(w.x & 0xFFFF0000u);
         v[i][2] = __uint_as_float(w.y << 16); v[i][3] = __uint_as_float(w.y & 0xFFFF0000u);
@@ -934,8 +938,12 @@ __global__ void __launch_bounds__(32) build_wide_kernel(BuildParams p, int B) {
     for (int i = 0; i < B; ++i) {
       const T *src = K + (int64_t)i * p.st;
       float v[4];
+      if constexpr (sizeof(T) == 1) {
+        load_codes(src, p.k_scale[(int64_t)block * p.Hkv + h], p.kvq_fmt, v);
+      } else {
 #pragma unroll
-      for (int c = 0; c < 4; ++c) v[c] = ldf<T>(src, c);
+        for (int c = 0; c < 4; ++c) v[c] = ldf<T>(src, c);
+      }
 #pragma unroll
       for (int c = 0; c < 4; ++c) { mu[c] += v[c]; knorm2 = fmaf(v[c], v[c], knorm2); }
       *reinterpret_cast<float4 *>(Ds + i * kWideDStride + 4 * lane) = make_float4(v[0], v[1], v[2], v[3]);
@@ -1155,6 +1163,7 @@ int locks_launch_build(locks_ctx *c, const locks_kv *kv, int batch, const int32_
   p.k_new = just_filled ? k_new : nullptr; p.append_pos = just_filled ? append_pos : nullptr;
   p.seq_commit = early ? seq_commit : nullptr; p.arrivals = c->arrivals;
   p.stage = early ? reinterpret_cast<uint8_t *>(c->stage_summ) : nullptr; p.staged = c->staged;
+  p.k_scale = nullptr; p.kvq_fmt = 0;
   p.hint = nullptr; p.kpages = c->k; p.hint_wpp = 1; p.hint_rounds = 1; p.hint_W = 1;
   if (just_filled && c->hint_dev && c->cfg.summary_fmt == LOCKS_FMT_I4 && c->cfg.q_dtype == LOCKS_BF16) {
     const locks_scan_geom geo = locks_scan_geometry(c, batch);
@@ -1224,4 +1233,46 @@ int locks_launch_build(locks_ctx *c, const locks_kv *kv, int batch, const int32_
   }
 #undef LOCKS_BUILD_CASE
   return locks_check_launch(c);
+}
+
+// Summaries from the codes of the 8-bit cache: the row-major kernels, which read a key's four dimensions as one word
+int locks_launch_build_codes(locks_ctx *c, const locks_kvq *kv, int batch, const int32_t *pb, const int32_t *pe, void *summaries, cudaStream_t st) {
+  BuildParams p = {};
+  p.k = kv->k; p.sb = kv->stride_block; p.sh = kv->stride_head; p.st = kv->stride_token;
+  p.block_table = kv->block_table; p.seq_lens = kv->seq_lens; p.page_begin = pb; p.page_end = pe;
+  p.summ = reinterpret_cast<uint8_t *>(summaries); p.status = c->status;
+  p.batch = batch; p.Hkv = c->cfg.num_kv_heads; p.Pmax = c->Pmax; p.num_blocks = kv->num_blocks;
+  p.r = c->cfg.rank; p.S = c->S; p.fmt = c->cfg.summary_fmt; p.esz = 1;
+  p.k_scale = kv->k_scale; p.kvq_fmt = kv->fmt;
+  const bool wide = c->B != LOCKS_B;
+  const int smem = wide ? build_wide_smem(c->B) : kBuildWarps * kBuildSmemPerWarp;
+  constexpr int kPer = kBuildWarps * kBuildItems;
+  const dim3 grid(wide ? c->Pmax : (c->Pmax + kPer - 1) / kPer, p.Hkv, batch);
+#define LOCKS_CODES_CASE(F_)                                                                                                             \
+  do {                                                                                                                                   \
+    if (wide) {                                                                                                                          \
+      if (locks_attrs_needed(LOCKS_ATTR_BUILD_CODES + F_))                                                                               \
+        cudaFuncSetAttribute(build_wide_kernel<uint8_t, F_>, cudaFuncAttributeMaxDynamicSharedMemorySize, build_wide_smem(64));          \
+      build_wide_kernel<uint8_t, F_><<<grid, 32, smem, st>>>(p, c->B);                                                                   \
+    } else {                                                                                                                             \
+      build_kernel<uint8_t, F_><<<grid, kBuildWarps * 32, smem, st>>>(p);                                                                \
+    }                                                                                                                                    \
+  } while (0)
+  switch (c->cfg.summary_fmt) {
+    case LOCKS_FMT_I4: LOCKS_CODES_CASE(LOCKS_FMT_I4); break;
+    case LOCKS_FMT_I8: LOCKS_CODES_CASE(LOCKS_FMT_I8); break;
+    case LOCKS_FMT_BF16: LOCKS_CODES_CASE(LOCKS_FMT_BF16); break;
+    default: LOCKS_CODES_CASE(LOCKS_FMT_F32); break;
+  }
+#undef LOCKS_CODES_CASE
+  return locks_check_launch(c);
+}
+
+extern "C" int locks_kvq_build_summaries(locks_ctx *ctx, const locks_kvq *kv, int batch, const int32_t *page_begin, const int32_t *page_end,
+                                         void *summaries, locks_stream stream) {
+  int rc = kvq_check(ctx, kv, batch);
+  if (rc != LOCKS_OK) return rc;
+  if (!summaries || ((uintptr_t)summaries % 16) || ((page_begin == nullptr) != (page_end == nullptr))) return LOCKS_ERR_INVALID_ARG;
+  ctx->last_launches = 0;
+  return locks_launch_build_codes(ctx, kv, batch, page_begin, page_end, summaries, (cudaStream_t)stream);
 }

@@ -1,7 +1,7 @@
 // Parameters and arithmetic shared by the summary-build kernels (build.cu: bulk; build_page.cu: the pages that a decode step
 // has just filled).
 #pragma once
-#include "locks_internal.cuh"
+#include "kvq.cuh"
 
 struct BuildParams {
   const void *k;
@@ -32,6 +32,9 @@ struct BuildParams {
   // bulk build of several layers in one launch: per-layer key caches and summary buffers (device arrays), or null
   const void *const *k_layers;
   void *const *summ_layers;
+  // build from the codes of the 8-bit cache: its scales [block][head] and LOCKS_KVQ_*; k and its strides are those of the codes
+  const float *k_scale;
+  int kvq_fmt;
 };
 
 // The pages that a decode step has just filled.  Adds its launch to c->last_launches.
@@ -46,6 +49,15 @@ int locks_launch_build_pages(locks_ctx *c, const BuildParams &p, cudaStream_t st
 __device__ __forceinline__ float inv_scale(float scale) { return scale == 0.f ? 0.f : __frcp_rn(scale); }
 __device__ __forceinline__ float round_code(float x, float inv, float qmax) {
   return fminf(fmaxf(rintf(x * inv), -qmax), qmax);
+}
+
+// four codes of the 8-bit cache as the values that they stand for
+__device__ __forceinline__ void load_codes(const uint8_t *src, float scale, int fmt, float (&v)[4]) {
+  uint32_t w = *reinterpret_cast<const uint32_t *>(src), lo, hi;
+  if (fmt == LOCKS_KVQ_INT) kvq_halves<LOCKS_KVQ_INT>(kvq_flip<LOCKS_KVQ_INT>(w), lo, hi);
+  else kvq_halves<LOCKS_KVQ_FLOAT>(w, lo, hi);
+  const float2 a = __half22float2(*reinterpret_cast<__half2 *>(&lo)), b = __half22float2(*reinterpret_cast<__half2 *>(&hi));
+  v[0] = a.x * scale; v[1] = a.y * scale; v[2] = b.x * scale; v[3] = b.y * scale;
 }
 
 // packed fp32 pairs (two independent lanes of arithmetic per instruction)

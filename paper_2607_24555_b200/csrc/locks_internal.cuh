@@ -89,6 +89,9 @@ struct locks_ctx {
   int32_t *arrivals;       // [max_batch] readers of a request's length that are done (zero between steps; see BuildParams)
   int32_t *staged;         // [max_batch][Hkv], behind arrivals: which of a staged summary's two parties have come (zero between steps)
   char *stage_summ;        // [max_batch][Hkv][S] summaries of a step that were ready before its scores
+  float *kvq_part;         // attention over the 8-bit cache: partials of problems that CTAs share, their (max, sum), arrivals (see kvq_attend.cu)
+  float2 *kvq_ml;
+  int32_t *kvq_done;
   cudaStream_t side;       // build of freshly filled pages, beside the whole step or from the end of the scan on
   cudaEvent_t ev_fork, ev_join;
   int last_launches;
@@ -219,8 +222,8 @@ static inline int locks_check_launch(locks_ctx *c) {
 // Function attributes (dynamic shared-memory limit, non-portable cluster size) belong to a device, not to the
 // process: true exactly once per (current device, kernel family), so that a process that drives several GPUs
 // sets them on each.  Thread-safe.
-enum { LOCKS_ATTR_SELECT = 0, LOCKS_ATTR_ATTEND = 1, LOCKS_ATTR_EXACT = 3, LOCKS_ATTR_SCAN = 8,
-       LOCKS_ATTR_BUILD_PAGE = 20 /* + page size / 32 */, LOCKS_ATTR_BUILD_WIDE = 24 /* + format */, LOCKS_ATTR_SCAN_WIDE = 28 /* + rank / 4 */ };
+enum { LOCKS_ATTR_SELECT = 0, LOCKS_ATTR_ATTEND = 1, LOCKS_ATTR_EXACT = 3, LOCKS_ATTR_KVQ = 4 /* + rows / 8 - 1, format */, LOCKS_ATTR_SCAN = 8,
+       LOCKS_ATTR_BUILD_PAGE = 20 /* + page size / 32 */, LOCKS_ATTR_BUILD_WIDE = 24 /* + format */, LOCKS_ATTR_SCAN_WIDE = 28 /* + rank / 4 */, LOCKS_ATTR_BUILD_CODES = 32 /* + format */ };
 bool locks_attrs_needed(int family);
 
 // ---------------------------------------------------------------- I4 blob geometry (d = 128; B = 16 unless given)

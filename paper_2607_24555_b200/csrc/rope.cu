@@ -1,0 +1,471 @@
+// Rotary positions (one axis or several), and appends of new tokens to the paged caches with the rotation on the way.
+//
+// A pair (a, b) of a head's dimensions turns by the angle position x frequency: (a cos - b sin, a sin + b cos).  Angles are formed in
+// fp64 turns (at position 10^6 the product's rounding to fp32 would be 0.03 rad), reduced to a fraction of a turn, and only then
+// go to fp32; rows are turned in fp32 and rounded once.  A token's cosines and sines are worked out once, in shared memory, for
+// all of its heads.
+#include <mutex>
+
+#include "kvq.cuh"
+
+namespace {
+
+struct Rows {   // strides in elements
+  const char *p;
+  int64_t st, sh;
+};
+
+__device__ __forceinline__ float2 turn(int pos, float inv_freq) {
+  double t = (double)pos * (double)inv_freq * 0.15915494309189533576888;   // turns: over 2 pi
+  t -= rint(t);
+  float s, c;
+  sincospif((float)(t + t), &s, &c);
+  return make_float2(c, s);
+}
+
+// eight consecutive dimensions
+__device__ __forceinline__ void load8(const __nv_bfloat16 *p, float *v) {
+  const uint4 w = *reinterpret_cast<const uint4 *>(p);
+  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = __uint_as_float(u[i] << 16);
+    v[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+  }
+}
+__device__ __forceinline__ void load8(const float *p, float *v) {
+  const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
+  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+__device__ __forceinline__ void store8(__nv_bfloat16 *p, const float *v) {
+  *reinterpret_cast<uint4 *>(p) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+}
+__device__ __forceinline__ void store8(float *p, const float *v) {
+  reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+  reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+
+// A head's 128 dimensions are eight units of 16: unit u < rot / 16 holds pairs 8 u .. 8 u + 7, the others what is not rotated.  A unit
+// is two runs of eight dimensions; where they begin:
+__device__ __forceinline__ void unit_runs(int u, int rot, int inter, int &lo, int &hi) {
+  if (inter || u >= rot / 16) { lo = 16 * u; hi = lo + 8; }
+  else { lo = 8 * u; hi = rot / 2 + lo; }
+}
+// v: the runs' values, cs: cosines and sines of the unit's pairs
+__device__ __forceinline__ void unit_turn(float (&v)[16], const float2 (&cs)[8], int inter) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float a = inter ? v[2 * i] : v[i], b = inter ? v[2 * i + 1] : v[8 + i];
+    const float x = fmaf(a, cs[i].x, -b * cs[i].y), y = fmaf(a, cs[i].y, b * cs[i].x);
+    if (inter) { v[2 * i] = x; v[2 * i + 1] = y; }
+    else { v[i] = x; v[8 + i] = y; }
+  }
+}
+
+struct RopeParams {
+  locks_rotary rot;
+  const int32_t *positions, *cu;
+  Rows q, qo, k, ko, v;      // ko: locks_rope only
+  int n, Hq, Hk, Hv, batch;  // Hq, Hk, Hv: heads of each that this call takes (0: none)
+  // the cache of locks_append_rows
+  char *kc, *vc;
+  int64_t sb, sh, st;
+  const int32_t *block_table, *seq_lens;
+  int num_blocks, Pmax, B;
+  int32_t *status;
+};
+
+// A CTA per token row: 16 heads at a time, each by eight threads of which one has a unit.  Bound by the chain of a few round trips
+// when there are few tokens (lengths and offsets; block; and rows, which are fetched meanwhile), by memory when there are many.
+constexpr int kRopeThreads = 128, kRopeAhead = 4;   // units that a thread has in flight
+
+template <typename T, bool APPEND>
+__global__ void __launch_bounds__(kRopeThreads) rope_rows_kernel(const __grid_constant__ RopeParams p) {
+  __shared__ float2 cs_s[64];
+  __shared__ int owner_s, pos_s, block_s;
+  const int tid = threadIdx.x, row = blockIdx.x, half = p.rot.rot_dim / 2, u = tid & 7;
+  const bool turns = p.rot.rot_dim > 0;
+  float inv = 0.f;
+  int axis = 0;
+  if (tid < half) { inv = p.rot.inv_freq[tid]; axis = p.rot.axis[tid]; }
+  int lo, hi;
+  unit_runs(u, p.rot.rot_dim, p.rot.interleaved, lo, hi);
+  const int heads = p.Hq + p.Hk + p.Hv;
+  pdl_trigger();
+  pdl_wait();
+  int pos = 0, len = 0;
+  if (p.positions && tid < half) pos = p.positions[(int64_t)axis * p.n + row];
+  auto src = [&](int h) -> const T * {
+    const Rows &r = h < p.Hq ? p.q : (h < p.Hq + p.Hk ? p.k : p.v);
+    const int hh = h < p.Hq ? h : (h < p.Hq + p.Hk ? h - p.Hq : h - p.Hq - p.Hk);
+    return reinterpret_cast<const T *>(r.p) + (int64_t)row * r.st + (int64_t)hh * r.sh;
+  };
+  float x[kRopeAhead][16];
+  auto fetch = [&](int h0) {
+#pragma unroll
+    for (int i = 0; i < kRopeAhead; ++i) {
+      const int h = h0 + (tid >> 3) + 16 * i;
+      if (h < heads) {
+        const T *s = src(h);
+        load8(s + lo, x[i]);
+        load8(s + hi, x[i] + 8);
+      }
+    }
+  };
+  if (APPEND) {
+    // whose row this is: the request with cu[b] <= row < cu[b + 1]
+    if (tid == 0) owner_s = -1;
+    __syncthreads();
+    if (!p.cu) {
+      if (tid == 0) {
+        len = p.seq_lens[row];
+        pos_s = len - 1;
+        if (len != 0) owner_s = row;   // (a length of zero: no token)
+      }
+    } else {
+      for (int b = tid; b < p.batch; b += kRopeThreads) {
+        const int c0 = p.cu[b], c1 = p.cu[b + 1];
+        len = p.seq_lens[b];
+        if (c0 <= row && row < c1) { owner_s = b; pos_s = (int)max((int64_t)len - c1 + row, (int64_t)-1); if (c1 - c0 > len) pos_s = -1; }
+      }
+    }
+    fetch(0);
+    __syncthreads();
+    if (owner_s < 0) return;   // a row behind the last request's
+    if (tid == 0) {
+      const int at = pos_s, page = at < 0 ? -1 : at / p.B;
+      int block = -1;
+      if (page >= 0 && page < p.Pmax) block = p.block_table[(int64_t)owner_s * p.Pmax + page];
+      if (block < 0 || block >= p.num_blocks) { block = -1; set_status(p.status, LOCKS_ERR_BAD_BLOCK); }
+      block_s = block;
+    }
+    if (!p.positions) pos = pos_s;
+  } else {
+    fetch(0);
+  }
+  if (tid < half) cs_s[tid] = turn(pos, inv);
+  __syncthreads();
+  float2 cs[8];
+  const bool mine = u < p.rot.rot_dim / 16;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) cs[i] = mine ? cs_s[8 * u + i] : make_float2(1.f, 0.f);
+  for (int h0 = 0; h0 < heads; h0 += 16 * kRopeAhead) {
+    if (h0) fetch(h0);
+#pragma unroll
+    for (int i = 0; i < kRopeAhead; ++i) {
+      const int h = h0 + (tid >> 3) + 16 * i;
+      if (h >= heads) break;
+      if (turns && mine && h < p.Hq + p.Hk) unit_turn(x[i], cs, p.rot.interleaved);
+      T *d;
+      if (h < p.Hq) {
+        d = reinterpret_cast<T *>(const_cast<char *>(p.qo.p)) + (int64_t)row * p.qo.st + (int64_t)h * p.qo.sh;
+      } else if (!APPEND) {
+        d = reinterpret_cast<T *>(const_cast<char *>(p.ko.p)) + (int64_t)row * p.ko.st + (int64_t)(h - p.Hq) * p.ko.sh;
+      } else {
+        if (block_s < 0) continue;
+        const bool key = h < p.Hq + p.Hk;
+        const int hh = h - p.Hq - (key ? 0 : p.Hk);
+        d = reinterpret_cast<T *>(key ? p.kc : p.vc) + (int64_t)block_s * p.sb + (int64_t)hh * p.sh + (int64_t)(pos_s % p.B) * p.st;
+      }
+      store8(d + lo, x[i]);
+      store8(d + hi, x[i] + 8);
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ the 8-bit cache
+struct QAppendParams {
+  locks_rotary rot;
+  const int32_t *positions, *cu;
+  Rows q, qo, k, v;
+  int n, Hq, batch;
+  KvqCache c;
+  int32_t *status;
+};
+
+constexpr int kMostTokens = 1 << 30;   // places stay far from 32 bits' end
+constexpr int kQWarps = 8, kQThreads = kQWarps * 32;
+
+template <int FMT> __device__ __forceinline__ uint32_t code4(const float *v, float scale) {   // true quotients, rounded to even
+  if (FMT == LOCKS_KVQ_INT) {
+    int c[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c[i] = __float2int_rn(fminf(fmaxf(__fdiv_rn(v[i], scale), -127.f), 127.f));
+    return (uint32_t)(c[0] & 255) | (uint32_t)(c[1] & 255) << 8 | (uint32_t)(c[2] & 255) << 16 | (uint32_t)(c[3] & 255) << 24;
+  }
+  uint16_t lo, hi;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(__fdiv_rn(v[1], scale)), "f"(__fdiv_rn(v[0], scale)));
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(__fdiv_rn(v[3], scale)), "f"(__fdiv_rn(v[2], scale)));
+  return (uint32_t)lo | (uint32_t)hi << 16;
+}
+
+// A CTA per (request, page that gets tokens and is complete afterwards), all KV heads; the first of a request's also takes its
+// unfinished last page, whose tokens replace the tail that the first page has been put together from.  A warp has 16 tokens of a
+// head's keys or values in registers (a lane: a unit of four tokens), so that the largest magnitude is known before a code is
+// written and everything is read once; pages of 32 and 64 tokens are two and four warps' work.  The CTA's cosines and sines serve
+// all heads, and the query rows of its tokens.
+template <int FMT>
+__global__ void __launch_bounds__(kQThreads) kvq_append_kernel(const __grid_constant__ QAppendParams p) {
+  extern __shared__ float2 cs_s[];   // [B][64]
+  __shared__ int found_s[4];         // request, item of it, first row, new tokens
+  __shared__ int warp_s[kQWarps];
+  __shared__ uint32_t amax_s[kQWarps];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, B = p.c.B;
+  const int half = p.rot.rot_dim / 2, u = lane & 7, inter = p.rot.interleaved;
+  int lo, hi;
+  unit_runs(u, p.rot.rot_dim, inter, lo, hi);
+  const bool mine = u < p.rot.rot_dim / 16;
+  pdl_trigger();
+  pdl_wait();
+  int b = blockIdx.x, item = 0, row0 = b, n = 1;
+  if (p.cu) {
+    // the request that this CTA's item belongs to: a running sum of the requests' items
+    if (tid == 0) found_s[0] = -1;
+    int before = 0;
+    for (int b0 = 0; b0 < p.batch; b0 += kQThreads) {
+      const int i = b0 + tid;
+      int items = 0, c0 = 0, m = 0;
+      if (i < p.batch) {
+        c0 = p.cu[i];
+        m = p.cu[i + 1] - c0;
+        const int T = p.c.seq_lens[i];
+        if (m != 0 && (m < 0 || m > T || T > kMostTokens || c0 < 0 || c0 > p.n - m)) {
+          set_status(p.status, LOCKS_ERR_BAD_BLOCK);
+          m = 0;
+        }
+        if (m > 0) items = max(1, T / B - (T - m) / B);
+      }
+      int sum = items;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, sum, o);
+        if (lane >= o) sum += x;
+      }
+      if (lane == 31) warp_s[warp] = sum;
+      __syncthreads();
+      int all = 0;
+#pragma unroll
+      for (int w = 0; w < kQWarps; ++w) {
+        if (w < warp) sum += warp_s[w];
+        all += warp_s[w];
+      }
+      const int at = (int)blockIdx.x - before - (sum - items);
+      if (at >= 0 && at < items) { found_s[0] = i; found_s[1] = at; found_s[2] = c0; found_s[3] = m; }
+      before += all;
+      __syncthreads();
+      if (before > (int)blockIdx.x && blockIdx.x + 1 < gridDim.x) break;   // (the last CTA looks at every request)
+    }
+    if (found_s[0] < 0) return;
+    b = found_s[0]; item = found_s[1]; row0 = found_s[2]; n = found_s[3];
+  }
+  const int T = p.c.seq_lens[b], start = T - n;
+  if (start < 0 || T > kMostTokens) {   // (one token per request: none at a length of zero)
+    if (tid == 0 && T != 0) set_status(p.status, LOCKS_ERR_BAD_BLOCK);
+    return;
+  }
+  const int sub_shift = B == 64 ? 2 : (B == 32 ? 1 : 0);   // a page is 2^sub_shift warps' work
+  auto do_page = [&](int page) {
+    const int first = page * B, t0 = max(first, start), t1 = min(first + B, T);
+    const bool complete = first + B <= T;
+    for (int i = tid; i < (t1 - t0) * half; i += kQThreads) {
+      const int t = i / half, f = i - t * half, row = row0 + t0 + t - start;
+      cs_s[t * 64 + f] = turn(p.positions ? p.positions[(int64_t)p.rot.axis[f] * p.n + row] : t0 + t, p.rot.inv_freq[f]);
+    }
+    int block = -1;
+    if (complete) {
+      if (page < p.c.Pmax) block = p.c.block_table[(int64_t)b * p.c.Pmax + page];
+      if (block < 0 || block >= p.c.num_blocks) {
+        block = -1;
+        if (tid == 0) set_status(p.status, LOCKS_ERR_BAD_BLOCK);
+      }
+    }
+    const bool fits = page < p.c.Pmax;
+    if (!fits && !complete && tid == 0) set_status(p.status, LOCKS_ERR_BAD_BLOCK);
+    __syncthreads();
+    auto turned = [&](float (&x)[16], int t) {   // t: token of this page's new ones
+      float2 cs[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) cs[i] = cs_s[t * 64 + 8 * u + i];
+      unit_turn(x, cs, inter);
+    };
+    // ---- keys and values
+    const int tasks = 2 * p.c.Hkv, per_round = kQWarps >> sub_shift, sub = warp & ((1 << sub_shift) - 1);
+    for (int r = 0; r < tasks; r += per_round) {
+      const int task = r + (warp >> sub_shift), h = task >> 1;
+      const bool live = task < tasks, key = !(task & 1);
+      const int64_t tail0 = ((int64_t)b * p.c.Hkv + h) * B;
+      float *tail = (key ? p.c.kt : p.c.vt) + tail0 * LOCKS_D;
+      const Rows &src = key ? p.k : p.v;
+      float x[4][16];
+      uint32_t amax = 0;
+      if (live) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int pos = first + 16 * sub + 4 * i + (lane >> 3);
+          if (pos < t0) {
+            if (complete) { load8(tail + (pos - first) * LOCKS_D + lo, x[i]); load8(tail + (pos - first) * LOCKS_D + hi, x[i] + 8); }
+          } else if (pos < t1) {
+            const __nv_bfloat16 *s = reinterpret_cast<const __nv_bfloat16 *>(src.p) + (int64_t)(row0 + pos - start) * src.st + (int64_t)h * src.sh;
+            load8(s + lo, x[i]);
+            load8(s + hi, x[i] + 8);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int pos = first + 16 * sub + 4 * i + (lane >> 3);
+          if (key && mine && pos >= t0 && pos < t1) turned(x[i], pos - t0);
+        }
+      }
+      if (complete) {
+        if (live) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) amax = max(amax, __float_as_uint(x[i][e]) & 0x7fffffffu);   // (ordered as magnitudes, NaN last)
+        }
+        amax = __reduce_max_sync(0xffffffffu, amax);
+        if (sub_shift) {
+          if (lane == 0) amax_s[warp] = amax;
+          __syncthreads();
+          const int w0 = warp & ~((1 << sub_shift) - 1);
+          for (int w = 0; w < 1 << sub_shift; ++w) amax = max(amax, amax_s[w0 + w]);
+          __syncthreads();
+        }
+        if (live && block >= 0) {
+          float scale = __fdiv_rn(__uint_as_float(amax), FMT == LOCKS_KVQ_INT ? 127.f : 448.f);
+          const bool codes = amax >= KVQ_TINY_BITS && amax < 0x7f800000u;
+          if (!codes) scale = amax < KVQ_TINY_BITS ? 0.f : __uint_as_float(0x7fffffffu);
+          char *dst = (key ? p.c.k : p.c.v) + (int64_t)block * p.c.sb + (int64_t)h * p.c.sh;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            char *d = dst + (int64_t)(16 * sub + 4 * i + (lane >> 3)) * p.c.st;
+            const uint2 a = codes ? make_uint2(code4<FMT>(x[i], scale), code4<FMT>(x[i] + 4, scale)) : make_uint2(0, 0);
+            const uint2 c = codes ? make_uint2(code4<FMT>(x[i] + 8, scale), code4<FMT>(x[i] + 12, scale)) : make_uint2(0, 0);
+            *reinterpret_cast<uint2 *>(d + lo) = a;
+            *reinterpret_cast<uint2 *>(d + hi) = c;
+          }
+          if (lane == 0 && sub == 0) (key ? p.c.ks : p.c.vs)[(int64_t)block * p.c.Hkv + h] = scale;
+        }
+      } else if (live && fits) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int pos = first + 16 * sub + 4 * i + (lane >> 3);
+          if (pos >= t0 && pos < t1) { store8(tail + (pos - first) * LOCKS_D + lo, x[i]); store8(tail + (pos - first) * LOCKS_D + hi, x[i] + 8); }
+        }
+      }
+    }
+    // ---- query rows of the page's new tokens
+    if (p.qo.p) {
+      const int rows = (t1 - t0) * p.Hq;
+      for (int r = tid >> 3; r < rows; r += kQThreads / 8) {
+        const int t = r / p.Hq, h = r - t * p.Hq;
+        const int64_t row = row0 + t0 + t - start;
+        const __nv_bfloat16 *s = reinterpret_cast<const __nv_bfloat16 *>(p.q.p) + row * p.q.st + (int64_t)h * p.q.sh;
+        __nv_bfloat16 *d = reinterpret_cast<__nv_bfloat16 *>(const_cast<char *>(p.qo.p)) + row * p.qo.st + (int64_t)h * p.qo.sh;
+        float x[16];
+        load8(s + lo, x);
+        load8(s + hi, x + 8);
+        if (mine) turned(x, t);
+        store8(d + lo, x);
+        store8(d + hi, x + 8);
+      }
+    }
+  };
+  const int p0 = start / B, last = T / B;
+  do_page(p0 + item);
+  if (item == 0 && last != p0 && T % B) {
+    __syncthreads();   // the tail's old tokens have been read, the cosines used
+    do_page(last);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ host
+int rows_ok(const locks_ctx *c, const locks_rows *r) {
+  if (!r->p || (uintptr_t)r->p % 16) return 0;
+  const int64_t m = c->cfg.kv_dtype == LOCKS_BF16 ? 8 : 4;
+  return r->stride_token % m == 0 && r->stride_head % m == 0;
+}
+Rows rows(const locks_rows *r) {
+  return r ? Rows{reinterpret_cast<const char *>(r->p), r->stride_token, r->stride_head} : Rows{nullptr, 0, 0};
+}
+
+int rotary_ok(const locks_rotary *r) {
+  if (r->rot_dim < 16 || r->rot_dim > LOCKS_D || r->rot_dim % 16 || r->num_axes < 1 || r->num_axes > LOCKS_MAX_AXES) return LOCKS_ERR_INVALID_ARG;
+  if (r->interleaved != 0 && r->interleaved != 1) return LOCKS_ERR_INVALID_ARG;
+  for (int i = 0; i < r->rot_dim / 2; ++i)
+    if (r->axis[i] >= r->num_axes || !std::isfinite(r->inv_freq[i])) return LOCKS_ERR_INVALID_ARG;
+  return LOCKS_OK;
+}
+
+// what the two appends check alike
+int append_ok(const locks_ctx *c, const locks_rotary *rot, const int32_t *cu, int n, const locks_rows *q, const locks_rows *qo,
+              const locks_rows *k, const locks_rows *v, int batch) {
+  if (!c || !k || !v || !rows_ok(c, k) || !rows_ok(c, v) || n < 1 || (!cu && n != batch)) return LOCKS_ERR_INVALID_ARG;
+  if ((q == nullptr) != (qo == nullptr) || (q && (!rot || !rows_ok(c, q) || !rows_ok(c, qo)))) return LOCKS_ERR_INVALID_ARG;
+  return rot ? rotary_ok(rot) : LOCKS_OK;
+}
+
+}  // namespace
+
+extern "C" int locks_rope(locks_ctx *ctx, const locks_rotary *rot, const int32_t *positions, int num_tokens, const locks_rows *q,
+                          const locks_rows *q_out, const locks_rows *k, const locks_rows *k_out, locks_stream stream) {
+  if (!ctx || !rot || !positions || num_tokens < 1) return LOCKS_ERR_INVALID_ARG;
+  if ((q == nullptr) != (q_out == nullptr) || (k == nullptr) != (k_out == nullptr) || (!q && !k)) return LOCKS_ERR_INVALID_ARG;
+  for (const locks_rows *r : {q, q_out, k, k_out})
+    if (r && !rows_ok(ctx, r)) return LOCKS_ERR_INVALID_ARG;
+  int rc = rotary_ok(rot);
+  if (rc != LOCKS_OK) return rc;
+  RopeParams p = {};
+  p.rot = *rot; p.positions = positions; p.n = num_tokens;
+  p.q = rows(q); p.qo = rows(q_out); p.k = rows(k); p.ko = rows(k_out);
+  p.Hq = q ? ctx->cfg.num_q_heads : 0; p.Hk = k ? ctx->cfg.num_kv_heads : 0;
+  ctx->last_launches = 0;
+  if (ctx->cfg.kv_dtype == LOCKS_BF16) locks_launch_pdl(rope_rows_kernel<__nv_bfloat16, false>, dim3(num_tokens), dim3(kRopeThreads), 0, (cudaStream_t)stream, p);
+  else locks_launch_pdl(rope_rows_kernel<float, false>, dim3(num_tokens), dim3(kRopeThreads), 0, (cudaStream_t)stream, p);
+  return locks_check_launch(ctx);
+}
+
+extern "C" int locks_append_rows(locks_ctx *ctx, const locks_rotary *rot, const int32_t *positions, const int32_t *cu_tokens, int num_tokens,
+                            const locks_rows *q, const locks_rows *q_out, const locks_rows *k_new, const locks_rows *v_new,
+                            const locks_kv *kv, int batch, locks_stream stream) {
+  if (!ctx || !kv || !kv->k || !kv->v || !kv->block_table || !kv->seq_lens) return LOCKS_ERR_INVALID_ARG;
+  if (batch <= 0 || batch > ctx->cfg.max_batch || kv->num_blocks <= 0) return LOCKS_ERR_INVALID_ARG;
+  if (kv->stride_block <= 0 || kv->stride_head <= 0 || kv->stride_token < LOCKS_D) return LOCKS_ERR_INVALID_ARG;
+  if ((kv->stride_block | kv->stride_head | kv->stride_token) % (ctx->cfg.kv_dtype == LOCKS_BF16 ? 8 : 4)) return LOCKS_ERR_INVALID_ARG;
+  if (((uintptr_t)kv->k | (uintptr_t)kv->v) % 16) return LOCKS_ERR_INVALID_ARG;
+  int rc = append_ok(ctx, rot, cu_tokens, num_tokens, q, q_out, k_new, v_new, batch);
+  if (rc != LOCKS_OK) return rc;
+  RopeParams p = {};
+  if (rot) p.rot = *rot;
+  p.positions = positions; p.cu = cu_tokens; p.n = num_tokens; p.batch = batch;
+  p.q = rows(q); p.qo = rows(q_out); p.k = rows(k_new); p.v = rows(v_new);
+  p.Hq = q ? ctx->cfg.num_q_heads : 0; p.Hk = p.Hv = ctx->cfg.num_kv_heads;
+  p.kc = reinterpret_cast<char *>(kv->k); p.vc = reinterpret_cast<char *>(kv->v);
+  p.sb = kv->stride_block; p.sh = kv->stride_head; p.st = kv->stride_token;
+  p.block_table = kv->block_table; p.seq_lens = kv->seq_lens; p.num_blocks = kv->num_blocks; p.Pmax = ctx->Pmax; p.B = ctx->B;
+  p.status = ctx->status;
+  ctx->last_launches = 0;
+  if (ctx->cfg.kv_dtype == LOCKS_BF16) locks_launch_pdl(rope_rows_kernel<__nv_bfloat16, true>, dim3(num_tokens), dim3(kRopeThreads), 0, (cudaStream_t)stream, p);
+  else locks_launch_pdl(rope_rows_kernel<float, true>, dim3(num_tokens), dim3(kRopeThreads), 0, (cudaStream_t)stream, p);
+  return locks_check_launch(ctx);
+}
+
+extern "C" int locks_kvq_append(locks_ctx *ctx, const locks_rotary *rot, const int32_t *positions, const int32_t *cu_tokens, int num_tokens,
+                                const locks_rows *q, const locks_rows *q_out, const locks_rows *k_new, const locks_rows *v_new,
+                                const locks_kvq *kv, int batch, locks_stream stream) {
+  int rc = kvq_check(ctx, kv, batch);
+  if (rc != LOCKS_OK) return rc;
+  if ((rc = append_ok(ctx, rot, cu_tokens, num_tokens, q, q_out, k_new, v_new, batch)) != LOCKS_OK) return rc;
+  QAppendParams p = {};
+  if (rot) p.rot = *rot;
+  p.positions = positions; p.cu = cu_tokens; p.n = num_tokens; p.batch = batch;
+  p.q = rows(q); p.qo = rows(q_out); p.k = rows(k_new); p.v = rows(v_new);
+  p.Hq = ctx->cfg.num_q_heads; p.c = kvq_cache(ctx, kv); p.status = ctx->status;
+  // a request with m new tokens completes at most (m + B - 1) / B pages, and has an item at least
+  const int64_t grid = cu_tokens ? (int64_t)num_tokens / ctx->B + batch : batch;
+  const size_t smem = (size_t)ctx->B * 64 * sizeof(float2);
+  ctx->last_launches = 0;
+  if (kv->fmt == LOCKS_KVQ_INT) locks_launch_pdl(kvq_append_kernel<LOCKS_KVQ_INT>, dim3((unsigned)grid), dim3(kQThreads), smem, (cudaStream_t)stream, p);
+  else locks_launch_pdl(kvq_append_kernel<LOCKS_KVQ_FLOAT>, dim3((unsigned)grid), dim3(kQThreads), smem, (cudaStream_t)stream, p);
+  return locks_check_launch(ctx);
+}
