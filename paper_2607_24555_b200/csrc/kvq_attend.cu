@@ -1,17 +1,24 @@
 // Attention over the 8-bit paged cache, for single tokens and a few tokens per request:
 //   o_r = sum_i softmax_i(q_r . k_i s_k(i) sm_scale) v_i s_v(i)   over the tokens i that row r sees.
 //
-// Codes are whole numbers (or e4m3 numbers) that fp16 holds exactly, so both products run on the tensor cores in fp16: a query row goes
-// in times a power of two that brings its largest element to 1 .. 2 (exact, and undone on the scores in fp32), a page's key scale
-// is a factor of its 16 scores, and P V of a tile starts from zero and joins the fp32 output by one rounding multiply-add with the
-// page's value scale, so that no scale meets fp16's range.  P is rounded to fp16 (2^-12 of each weight; the sum of the weights
-// is that of the unrounded ones).  Scores, maxima, sums and outputs are fp32.
+// Codes are numbers that fp16 holds exactly, so both products run on the tensor cores in fp16.  A query row goes in times a power of
+// two that brings its largest element to 1 .. 2 (exact, and undone on the scores in fp32), a page's key scale is a factor of its
+// scores, and P V of 16 tokens joins the fp32 output by one rounding multiply-add with the page's value scale, so that no scale meets
+// fp16's range.  Weights go in as 2^15 p in fp16 (within 2^-11 of each, and normal down to p = 2^-29); the sum that divides is that of
+// the unrounded ones.  Scores, maxima, sums and outputs are fp32.
 //
-// A problem is a (request, KV head, row tile): up to 8 or 16 query rows, the G heads of one or several tokens.  The 16-token tiles of all problems
-// form one line that is cut into equal shares, one per CTA, whatever the lengths: a CTA's share is a few segments of problems, and
-// a problem that several CTAs share is put together by the last of them.  A warp streams every fourth tile of a segment from global
-// memory straight into MMA fragments, a tile ahead: the order of dimensions in q k and of tokens and dimensions in p v is free, and is
-// chosen such that a lane's bytes are 16-byte pieces of rows.
+// Signed codes: byte u = code + 128 (its sign bit flipped) with a zero byte above it is the fp16 number 2^-24 u, without any
+// arithmetic.  So the products are those of u, and what 128 adds to them, 128 sum_d q_d and 128 sum_i p_i, is taken off by the
+// accumulators' start: the first is known once per row, the second is one more MMA, with ones for values.  (As differences of
+// numbers 1024 + u and 1152 the conversions were 176 of a tile's 500 instructions; 8 x 32K tokens took 116 us.)
+//
+// A problem is a (request, KV head, row tile): up to 8 or 16 query rows, the G heads of one or several tokens.  The pairs of 16-token tiles
+// of all problems form one line that is cut into equal shares, one per CTA, whatever the lengths: a CTA's share is a few segments of
+// problems, and a problem that several CTAs share is put together by the last of them, or by a second kernel where they are many.
+// A warp streams every fourth pair of a segment through a ring in shared memory and reads it as MMA fragments: the order of
+// dimensions in q k and of tokens and dimensions in p v is free, and is chosen such that a lane's bytes are 16-byte pieces of rows.
+#include <algorithm>
+
 #include "kvq.cuh"
 
 namespace {
@@ -19,7 +26,10 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kRowPad = LOCKS_D + 4;   // floats of a row of a warp's partial
-constexpr int kMinShare = 2 * kWarps;  // tiles of a share at least: two per warp
+constexpr int kUnfinished = -2;        // in a block's place: the unfinished page
+constexpr int kManyShares = 16;        // CTAs per problem from which on the partials are put together by a second kernel
+constexpr int kLead = 6;               // what a problem's start costs, in pairs: so many places of the line come before its pairs
+constexpr int kMinShare = kLead + kWarps;      // pairs of tiles of a share at least: one per warp
 
 struct QAttParams {
   const __nv_bfloat16 *q;
@@ -55,8 +65,8 @@ __device__ __forceinline__ void copy16(void *dst, const void *src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(smem_u32(dst)), "l"(src) : "memory");
 }
 
-// One request's share of the line: its tokens, its length, tiles of a problem, problems (row tiles x KV heads)
-struct Request { int T, n, row0, tiles, row_tiles; };
+// One request's part of the line: its length, tokens, first row, pairs of tiles of a problem, row tiles (problems: times KV heads)
+struct Request { int T, n, row0, pairs, row_tiles; };
 
 __device__ __forceinline__ Request request_at(const QAttParams &p, int b) {
   Request r;
@@ -72,57 +82,69 @@ __device__ __forceinline__ Request request_at(const QAttParams &p, int b) {
     }
   }
   if (p.ids) {
-    r.tiles = p.kbud << p.sub_shift;
+    r.pairs = ((p.kbud << p.sub_shift) + 1) >> 1;
   } else {
     int pages = r.T > 0 ? (r.T - 1) / p.c.B + 1 : 0;
     if (pages > p.c.Pmax) { set_status(p.status, LOCKS_ERR_BAD_BLOCK); pages = p.c.Pmax; }
-    r.tiles = max(pages << p.sub_shift, 1);   // (an empty sequence's problem writes its zeros all the same)
+    r.pairs = max(((pages << p.sub_shift) + 1) >> 1, 1);   // (an empty sequence's problem writes its zeros all the same)
   }
   r.row_tiles = (r.n + p.tile_tokens - 1) / p.tile_tokens;
   return r;
 }
 
-// The request that holds place u of the line: where its places begin.  All lanes of a warp take part.
-__device__ __forceinline__ bool find_request(const QAttParams &p, int64_t u, int lane, int &b, int64_t &begin, Request &req) {
-  int64_t before = 0;
-  for (int b0 = 0; b0 < p.batch; b0 += 32) {
-    const int i = b0 + lane;
-    Request r = {0, 0, 0, 0, 0};
-    if (i < p.batch) r = request_at(p, i);
-    const int64_t mine = (int64_t)r.tiles * r.row_tiles * p.Hkv;
-    int64_t sum = mine;
+__device__ __forceinline__ int places(const QAttParams &p, const Request &r) { return (kLead + r.pairs) * r.row_tiles * p.Hkv; }
+
+// 32 requests, a lane each: where their places end within the 32; the warp's total in lane 31
+__device__ __forceinline__ int scan_places(int mine, int lane) {
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int64_t x = __shfl_up_sync(0xffffffffu, sum, o);
-      if (lane >= o) sum += x;
-    }
-    const int64_t at = before + sum - mine;
-    const uint32_t has = __ballot_sync(0xffffffffu, u >= at && u < at + mine);
-    if (has) {
-      const int l = __ffs(has) - 1;
-      b = b0 + l;
-      begin = __shfl_sync(0xffffffffu, at, l);
-      req.T = __shfl_sync(0xffffffffu, r.T, l); req.n = __shfl_sync(0xffffffffu, r.n, l); req.row0 = __shfl_sync(0xffffffffu, r.row0, l);
-      req.tiles = __shfl_sync(0xffffffffu, r.tiles, l); req.row_tiles = __shfl_sync(0xffffffffu, r.row_tiles, l);
-      return true;
-    }
-    before += __shfl_sync(0xffffffffu, sum, 31);
+  for (int o = 1; o < 32; o <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, mine, o);
+    if (lane >= o) mine += x;
   }
-  return false;
-}
-__device__ __forceinline__ int64_t line_length(const QAttParams &p, int lane) {
-  int64_t all = 0;
-  for (int b0 = 0; b0 < p.batch; b0 += 32)
-    if (b0 + lane < p.batch) {
-      const Request r = request_at(p, b0 + lane);
-      all += (int64_t)r.tiles * r.row_tiles * p.Hkv;
-    }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
-  return all;
+  return mine;
 }
 
-__device__ __forceinline__ int64_t share_of(int64_t all) { return max((all + gridDim.x - 1) / (int64_t)gridDim.x, (int64_t)kMinShare); }
+// What a warp knows of the line: the first 32 requests (most batches: all), and the line's length.  (The host sees to it that the
+// length fits 32 bits.)
+struct Line {
+  Request r;        // lane: request
+  int end, all;     // lane: the end of its places
+  __device__ __forceinline__ void read(const QAttParams &p, int lane) {
+    r = Request{0, 0, 0, 0, 0};
+    if (lane < p.batch) r = request_at(p, lane);
+    end = scan_places(places(p, r), lane);
+    all = __shfl_sync(0xffffffffu, end, 31);
+    for (int b0 = 32; b0 < p.batch; b0 += 32) {
+      const int mine = b0 + lane < p.batch ? places(p, request_at(p, b0 + lane)) : 0;
+      all += __reduce_add_sync(0xffffffffu, mine);
+    }
+  }
+  // The request that holds place u (below `all`), and where its places begin
+  __device__ __forceinline__ void find(const QAttParams &p, int u, int lane, int &b, int &begin, Request &req) const {
+    Request x = r;
+    int to = end, at = to - places(p, x);
+    uint32_t has = __ballot_sync(0xffffffffu, u >= at && u < to);
+    b = 0;
+    while (!has && b + 32 < p.batch) {
+      const int before = __shfl_sync(0xffffffffu, to, 31);
+      b += 32;
+      x = Request{0, 0, 0, 0, 0};
+      if (b + lane < p.batch) x = request_at(p, b + lane);
+      to = before + scan_places(places(p, x), lane);
+      at = to - places(p, x);
+      has = __ballot_sync(0xffffffffu, u >= at && u < to);
+    }
+    const int l = has ? __ffs(has) - 1 : 0;
+    b += l;
+    begin = __shfl_sync(0xffffffffu, at, l);
+    req.T = __shfl_sync(0xffffffffu, x.T, l); req.n = __shfl_sync(0xffffffffu, x.n, l); req.row0 = __shfl_sync(0xffffffffu, x.row0, l);
+    req.pairs = __shfl_sync(0xffffffffu, x.pairs, l); req.row_tiles = __shfl_sync(0xffffffffu, x.row_tiles, l);
+  }
+};
+__device__ __forceinline__ int share_of(int all, int ctas) { return max((all - 1) / ctas + 1, kMinShare); }
+
+// Outputs are kept times 2^15 (of the weights) and this: the unit of signed codes' fp16 form; for e4m3, so that large scales stay in range
+template <int FMT> constexpr float kUnit = FMT == LOCKS_KVQ_INT ? 0x1p-24f : 0x1p-15f;
 
 // largest finite magnitude over a warp -> the power of two that brings it to 2^top .. 2^(top + 1)
 __device__ __forceinline__ float power_to(float amax, int top) {
@@ -135,9 +157,9 @@ __device__ __forceinline__ float finite_abs(float x) {
 }
 
 // The row tile's queries as A fragments: lane (x, t) holds four dims of row x (+ 8) per step, 64 (s / 4) + 16 t + 4 (s % 4) ..
-// Returns 2^-e c2, which undoes the power of two.
+// rs: what undoes the power of two, times c2; start: what signed codes' 128 adds to a row's sum of products, taken off.
 template <int NH>
-__device__ __forceinline__ void load_queries(const QAttParams &p, int64_t row0, int h, int rows, int x, int t, uint32_t (&qf)[NH][8][2], float (&rs)[NH]) {
+__device__ __forceinline__ void load_queries(const QAttParams &p, int64_t row0, int h, int rows, int x, int t, uint32_t (&qf)[NH][8][2], float (&rs)[NH], float (&start)[NH]) {
 #pragma unroll
   for (int hh = 0; hh < NH; ++hh) {
     const int r = x + 8 * hh, j = r / p.G, g = r - j * p.G;
@@ -166,15 +188,24 @@ __device__ __forceinline__ void load_queries(const QAttParams &p, int64_t row0, 
     amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
     const float up = power_to(amax, 0);
     rs[hh] = p.c2 / up;
+    float sum = 0.f;
+#pragma unroll
+    for (int s = 0; s < 8; ++s)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum += v[s][e] * up;
+    sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+    sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+    start[hh] = -0x1p-17f * sum;
 #pragma unroll
     for (int s = 0; s < 8; ++s) { qf[hh][s][0] = pack_f16(v[s][0] * up, v[s][1] * up); qf[hh][s][1] = pack_f16(v[s][2] * up, v[s][3] * up); }
   }
 }
 
-__device__ __forceinline__ void mma_f16_z(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};\n"
+// D = A B + C, with registers of its own for C (a start that several products share is not copied)
+__device__ __forceinline__ void mma_f16_from(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, float c0, float c1, float c2, float c3) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};\n"
       : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
 }
 
 // Running softmax of the row tile in a warp's registers
@@ -191,18 +222,26 @@ struct Running {
       for (int i = 0; i < 8; ++i) o[i][hh] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
   }
-  // Scores of tokens x, x + 8 of a tile -> weights of tokens 2 t, 2 t + 1, 8 + 2 t, 9 + 2 t (pw; as B fragments pb).  f[hh]: what
-  // the sums of products stand for, in log2 units; pos: place of the tile's first token; mask: some row does not see all of it
-  __device__ __forceinline__ void weights(const float (&s)[2][4], const float (&f)[NH], const int (&lim)[NH], int pos, bool mask, int t, uint32_t (&pb)[NH][2], float (&pw)[NH][4]) {
+  // Scores of H tiles (of tokens 2 t, 2 t + 1, 8 + 2 t, 9 + 2 t of each) -> weights times 2^15 (pw; as B fragments pb).  f: what the
+  // sums of products stand for, in log2 units.  mask: some row does not see all of the tile, whose first token's place is pos
+  template <int H, bool MASK>
+  __device__ __forceinline__ void weights(const float (&s)[2 * H][4], const float (&f)[H][NH], const int (&lim)[NH], int pos, int t, uint32_t (&pb)[H][NH][2], float (&pw)[H][NH][4]) {
 #pragma unroll
     for (int hh = 0; hh < NH; ++hh) {
-      float sv[4] = {s[0][2 * hh] * f[hh], s[0][2 * hh + 1] * f[hh], s[1][2 * hh] * f[hh], s[1][2 * hh + 1] * f[hh]};
-      if (mask) {
+      float sv[H][4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (pos + 2 * t + (e & 1) + 4 * (e & 2) >= lim[hh]) sv[e] = -INFINITY;
+      for (int w = 0; w < H; ++w)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          sv[w][e] = s[2 * w + (e >> 1)][2 * hh + (e & 1)];
+          if (MASK) sv[w][e] = pos + 2 * t + (e & 1) + 4 * (e & 2) >= lim[hh] ? -INFINITY : sv[w][e] * f[w][hh];
+        }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < H; ++w) {
+        const float m4 = fmaxf(fmaxf(sv[w][0], sv[w][1]), fmaxf(sv[w][2], sv[w][3]));
+        mx = fmaxf(mx, MASK ? m4 : m4 * f[w][hh]);
       }
-      float mx = fmaxf(fmaxf(sv[0], sv[1]), fmaxf(sv[2], sv[3]));
       mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
       mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
       const float mn = fmaxf(m[hh], mx), ms = mn == -INFINITY ? 0.f : mn;
@@ -214,50 +253,56 @@ struct Running {
         for (int i = 0; i < 8; ++i) { o[i][hh].x *= a0; o[i][hh].y *= a1; o[i][hh].z *= a0; o[i][hh].w *= a1; }
       }
       m[hh] = mn;
+      const float off = 15.f - ms;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) { pw[hh][e] = ex2f(sv[e] - ms); l[hh] += pw[hh][e]; }
-      pb[hh][0] = pack_f16(pw[hh][0], pw[hh][1]);
-      pb[hh][1] = pack_f16(pw[hh][2], pw[hh][3]);
+      for (int w = 0; w < H; ++w) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          pw[w][hh][e] = ex2f(MASK ? sv[w][e] + off : fmaf(sv[w][e], f[w][hh], off));
+          l[hh] += pw[w][hh][e];
+        }
+        pb[w][hh][0] = pack_f16(pw[w][hh][0], pw[w][hh][1]);
+        pb[w][hh][1] = pack_f16(pw[w][hh][2], pw[w][hh][3]);
+      }
     }
   }
-  // Two dims' values of the tile's tokens join the outputs, times f (of rows 2 t, 2 t + 1)
-  __device__ __forceinline__ void outputs(int i, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, const uint32_t (&pb)[NH][2], const float2 (&f)[NH]) {
+  // Two dims' values of a tile's tokens join the outputs, times f; start: the accumulators' (both of rows 2 t, 2 t + 1)
+  __device__ __forceinline__ void outputs(int i, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, const uint32_t (&pb)[NH][2], const float2 (&start)[NH], const float2 (&f)[NH]) {
 #pragma unroll
     for (int hh = 0; hh < NH; ++hh) {
       float c[4];
-      mma_f16_z(c, a0, a1, a2, a3, pb[hh][0], pb[hh][1]);
+      mma_f16_from(c, a0, a1, a2, a3, pb[hh][0], pb[hh][1], start[hh].x, start[hh].y, start[hh].x, start[hh].y);
       const float2 lo = fma2(make_float2(c[0], c[1]), f[hh], make_float2(o[i][hh].x, o[i][hh].y));
       const float2 hi = fma2(make_float2(c[2], c[3]), f[hh], make_float2(o[i][hh].z, o[i][hh].w));
       o[i][hh] = make_float4(lo.x, lo.y, hi.x, hi.y);
     }
   }
-  // into the warp's partial: [rows][kRowPad] outputs, [rows] (max, sum); `times` over, joined to what is there
-  __device__ __forceinline__ void leave(float *wo, float2 *wml, int x, int t, bool join, float times) {
+  // into the warp's partial: [rows][kRowPad] outputs, [rows] (max, sum).  JOIN: `times` over, to what is there
+  template <bool JOIN>
+  __device__ __forceinline__ void leave(float *wo, float2 *wml, int x, int t, float times) {
 #pragma unroll
     for (int hh = 0; hh < NH; ++hh) {
-      float sum = l[hh];
+      float sum = l[hh], f_old = 0.f, f_new = 1.f, mn = m[hh];
       sum += __shfl_xor_sync(0xffffffffu, sum, 1);
       sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-      float f_old = 0.f, f_new = 1.f, mn = m[hh];
-      sum *= times;
-      if (join) {
+      if (JOIN) {
         const float2 old = wml[x + 8 * hh];
         mn = fmaxf(old.x, m[hh]);
         f_old = mn == -INFINITY ? 1.f : ex2f(old.x - mn);
-        f_new = mn == -INFINITY ? 1.f : ex2f(m[hh] - mn);
+        f_new = times * (mn == -INFINITY ? 1.f : ex2f(m[hh] - mn));
         sum = old.y * f_old + sum * f_new;
+        __syncwarp();
       }
-      f_new *= times;
-      __syncwarp();
       if (t == 0) wml[x + 8 * hh] = make_float2(mn, sum);
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        const float fo = __shfl_sync(0xffffffffu, f_old, 8 * t + 4 * c), fn = __shfl_sync(0xffffffffu, f_new, 8 * t + 4 * c);
         float *w = wo + (2 * t + c + 8 * hh) * kRowPad + 16 * x;
+        float fo = 0.f, fn = 1.f;
+        if (JOIN) { fo = __shfl_sync(0xffffffffu, f_old, 8 * t + 4 * c); fn = __shfl_sync(0xffffffffu, f_new, 8 * t + 4 * c); }
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
           float4 y = c ? make_float4(o[i][hh].y, o[i][hh].w, o[i + 1][hh].y, o[i + 1][hh].w) : make_float4(o[i][hh].x, o[i][hh].z, o[i + 1][hh].x, o[i + 1][hh].z);
-          if (join) {
+          if (JOIN) {
             const float4 z = *reinterpret_cast<const float4 *>(w + 2 * i);
             y = make_float4(fmaf(y.x, fn, z.x * fo), fmaf(y.y, fn, z.y * fo), fmaf(y.z, fn, z.z * fo), fmaf(y.w, fn, z.w * fo));
           }
@@ -268,41 +313,27 @@ struct Running {
   }
 };
 
-// 16 places of the unfinished page (fp32), from pos on, joined to the warp's partial `times` over.  Elements go to fp16 by a power of
-// two of the tile's largest (2^-11 of each).  Not part of the tile loop: its registers would be the loop's.
-template <int NH>
-__device__ __forceinline__ void tail_tile(const QAttParams &p, int64_t row0, int h, int rows, int T, const int (&lim)[NH], const float *kt, const float *vt, int pos, float times, float *wo, float2 *wml) {
+// 16 places of the unfinished page (fp32), from pos on, joined to the warp's partial `times` over.  Elements go to fp16 times a power
+// of two of the tile's largest, values rounded (2^-11 of each), keys in two parts.  Out of line: its registers would be the tile loop's.
+template <int NH, int FMT>
+__device__ __noinline__ void tail_tile(const QAttParams &p, int row0, int h, int rows, int T, int lim0, int lim1, const float *kt, const float *vt, int pos, float times, float *wo, float2 *wml) {
   const int lane = threadIdx.x & 31, x = lane >> 2, t = lane & 3;
-  uint32_t qf[NH][8][2], pb[NH][2];
-  float rs[NH], pw[NH][4], s[2][4], f[NH];
-  load_queries<NH>(p, row0, h, rows, x, t, qf, rs);
+  uint32_t qf[NH][8][2], pb[1][NH][2];
+  float rs[NH], none[NH], pw[1][NH][4], s[2][4], f[1][NH];
+  int lim[NH];
+  lim[0] = lim0;
+  lim[NH - 1] = NH == 1 ? lim0 : lim1;
   Running<NH> run;
   run.clear();
   float4 k[2][8];
-  float amax = 0.f;
 #pragma unroll
   for (int w = 0; w < 2; ++w)
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       k[w][i] = make_float4(0.f, 0.f, 0.f, 0.f);
       if (pos + x + 8 * w < T) k[w][i] = *reinterpret_cast<const float4 *>(kt + (x + 8 * w) * LOCKS_D + (i >> 2) * 64 + 16 * t + 4 * (i & 3));
-      amax = fmaxf(amax, fmaxf(fmaxf(finite_abs(k[w][i].x), finite_abs(k[w][i].y)), fmaxf(finite_abs(k[w][i].z), finite_abs(k[w][i].w))));
     }
-  float up = power_to(warp_max(amax), 14);
-#pragma unroll
-  for (int w = 0; w < 2; ++w) {
-    s[w][0] = s[w][1] = s[w][2] = s[w][3] = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      mma_f16(s[w], qf[0][i][0], NH == 2 ? qf[NH - 1][i][0] : 0u, qf[0][i][1], NH == 2 ? qf[NH - 1][i][1] : 0u, pack_f16(k[w][i].x * up, k[w][i].y * up), pack_f16(k[w][i].z * up, k[w][i].w * up));
-  }
-#pragma unroll
-  for (int hh = 0; hh < NH; ++hh) f[hh] = rs[hh] / up;
-  run.weights(s, f, lim, pos, true, t, pb, pw);
-  // values: 16 dims of tokens 2 t, 2 t + 1, 8 + 2 t, 9 + 2 t
-  float4 v[4][4];
-  amax = 0.f;
-  bool odd = false;   // an infinity or a NaN
+  float4 v[4][4];   // 16 dims of tokens 2 t, 2 t + 1, 8 + 2 t, 9 + 2 t
 #pragma unroll
   for (int e = 0; e < 4; ++e)
 #pragma unroll
@@ -310,19 +341,57 @@ __device__ __forceinline__ void tail_tile(const QAttParams &p, int64_t row0, int
       const int tok = 2 * t + (e & 1) + 4 * (e & 2);
       v[e][i] = make_float4(0.f, 0.f, 0.f, 0.f);
       if (pos + tok < T) v[e][i] = *reinterpret_cast<const float4 *>(vt + tok * LOCKS_D + 16 * x + 4 * i);
-      const float a = fmaxf(fmaxf(finite_abs(v[e][i].x), finite_abs(v[e][i].y)), fmaxf(finite_abs(v[e][i].z), finite_abs(v[e][i].w)));
-      amax = fmaxf(amax, a);
+    }
+  float amax = 0.f;
+#pragma unroll
+  for (int w = 0; w < 2; ++w)
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      amax = fmaxf(amax, fmaxf(fmaxf(finite_abs(k[w][i].x), finite_abs(k[w][i].y)), fmaxf(finite_abs(k[w][i].z), finite_abs(k[w][i].w))));
+  float up = power_to(warp_max(amax), 14);
+  load_queries<NH>(p, row0, h, rows, x, t, qf, rs, none);
+  bool odd = false;   // an infinity or a NaN
+#pragma unroll
+  for (int w = 0; w < 2; ++w)
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      odd |= !(fabsf(k[w][i].x) < INFINITY && fabsf(k[w][i].y) < INFINITY && fabsf(k[w][i].z) < INFINITY && fabsf(k[w][i].w) < INFINITY);
+  const bool finite_tile = !__any_sync(0xffffffffu, odd);
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    s[w][0] = s[w][1] = s[w][2] = s[w][3] = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {   // in two parts: 22 bits of each
+      const uint32_t a0 = qf[0][i][0], a1 = NH == 2 ? qf[NH - 1][i][0] : 0u, a2 = qf[0][i][1], a3 = NH == 2 ? qf[NH - 1][i][1] : 0u;
+      const float4 y = make_float4(k[w][i].x * up, k[w][i].y * up, k[w][i].z * up, k[w][i].w * up);
+      uint32_t lo = pack_f16(y.x, y.y), hi = pack_f16(y.z, y.w);
+      mma_f16(s[w], a0, a1, a2, a3, lo, hi);
+      const float2 l2 = __half22float2(*reinterpret_cast<__half2 *>(&lo)), h2 = __half22float2(*reinterpret_cast<__half2 *>(&hi));
+      const float4 rest = make_float4(y.x - l2.x, y.y - l2.y, y.z - h2.x, y.w - h2.y);
+      if (finite_tile) mma_f16(s[w], a0, a1, a2, a3, pack_f16(rest.x, rest.y), pack_f16(rest.z, rest.w));
+    }
+  }
+#pragma unroll
+  for (int hh = 0; hh < NH; ++hh) f[0][hh] = rs[hh] / up;
+  run.template weights<1, true>(s, f, lim, pos, t, pb, pw);
+  amax = 0.f;
+  odd = false;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      amax = fmaxf(amax, fmaxf(fmaxf(finite_abs(v[e][i].x), finite_abs(v[e][i].y)), fmaxf(finite_abs(v[e][i].z), finite_abs(v[e][i].w))));
       odd |= !(fabsf(v[e][i].x) < INFINITY && fabsf(v[e][i].y) < INFINITY && fabsf(v[e][i].z) < INFINITY && fabsf(v[e][i].w) < INFINITY);
     }
   up = power_to(warp_max(amax), 14);
   if (!__any_sync(0xffffffffu, odd)) {
-    float2 back[NH];
+    float2 back[NH], zero[NH];
 #pragma unroll
-    for (int hh = 0; hh < NH; ++hh) back[hh] = make_float2(1.f / up, 1.f / up);
+    for (int hh = 0; hh < NH; ++hh) { back[hh] = make_float2(kUnit<FMT> / up, kUnit<FMT> / up); zero[hh] = make_float2(0.f, 0.f); }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      run.outputs(2 * i, pack_f16(v[0][i].x * up, v[1][i].x * up), pack_f16(v[0][i].y * up, v[1][i].y * up), pack_f16(v[2][i].x * up, v[3][i].x * up), pack_f16(v[2][i].y * up, v[3][i].y * up), pb, back);
-      run.outputs(2 * i + 1, pack_f16(v[0][i].z * up, v[1][i].z * up), pack_f16(v[0][i].w * up, v[1][i].w * up), pack_f16(v[2][i].z * up, v[3][i].z * up), pack_f16(v[2][i].w * up, v[3][i].w * up), pb, back);
+      run.outputs(2 * i, pack_f16(v[0][i].x * up, v[1][i].x * up), pack_f16(v[0][i].y * up, v[1][i].y * up), pack_f16(v[2][i].x * up, v[3][i].x * up), pack_f16(v[2][i].y * up, v[3][i].y * up), pb[0], zero, back);
+      run.outputs(2 * i + 1, pack_f16(v[0][i].z * up, v[1][i].z * up), pack_f16(v[0][i].w * up, v[1][i].w * up), pack_f16(v[2][i].z * up, v[3][i].z * up), pack_f16(v[2][i].w * up, v[3][i].w * up), pb[0], zero, back);
     }
   } else {   // token by token in fp32, so that a row takes nothing of a token that it does not see
 #pragma unroll 1
@@ -330,7 +399,7 @@ __device__ __forceinline__ void tail_tile(const QAttParams &p, int64_t row0, int
       const int e = (k2 & 1) + (k2 >> 3) * 2, from = (k2 & 7) >> 1;   // the weight's place: element e of the lanes with t = from
 #pragma unroll
       for (int hh = 0; hh < NH; ++hh) {
-        const float w = e == 0 ? pw[hh][0] : (e == 1 ? pw[hh][1] : (e == 2 ? pw[hh][2] : pw[hh][3]));
+        const float w = kUnit<FMT> * (e == 0 ? pw[0][hh][0] : (e == 1 ? pw[0][hh][1] : (e == 2 ? pw[0][hh][2] : pw[0][hh][3])));
         const float w0 = __shfl_sync(0xffffffffu, w, 8 * t + from), w1 = __shfl_sync(0xffffffffu, w, 8 * t + 4 + from);
         const bool s0 = pos + k2 < __shfl_sync(0xffffffffu, lim[hh], 8 * t), s1 = pos + k2 < __shfl_sync(0xffffffffu, lim[hh], 8 * t + 4);
 #pragma unroll
@@ -342,27 +411,65 @@ __device__ __forceinline__ void tail_tile(const QAttParams &p, int64_t row0, int
       }
     }
   }
-  run.leave(wo, wml, x, t, true, times);
+  run.template leave<true>(wo, wml, x, t, times);
+}
+
+// Partials of CTAs c, c + step, .. c1 of the problem that begins in CTA c0: row r, four dims; loads four at a time
+__device__ __forceinline__ float4 join_partials(const QAttParams &p, int c0, int c, int c1, int step, int r, int d4, float &M, float &L) {
+  M = -INFINITY;
+  L = 0.f;
+  float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (; c <= c1; c += 4 * step) {
+    float2 ml[4];
+    float4 y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int ci = c + i * step, s = 2 * ci + (ci == c0 ? 1 : 0);
+      ml[i] = make_float2(-INFINITY, 0.f);
+      y[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (ci <= c1) {
+        ml[i] = __ldcg(p.part_ml + s * KVQ_ROWS + r);
+        y[i] = __ldcg(reinterpret_cast<const float4 *>(p.part + ((int64_t)s * KVQ_ROWS + r) * LOCKS_D + d4));
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float mn = fmaxf(M, ml[i].x), fo = mn == -INFINITY ? 1.f : ex2f(M - mn), fn = mn == -INFINITY ? 1.f : ex2f(ml[i].x - mn);
+      L = L * fo + ml[i].y * fn;
+      a.x = a.x * fo + y[i].x * fn; a.y = a.y * fo + y[i].y * fn; a.z = a.z * fo + y[i].z * fn; a.w = a.w * fo + y[i].w * fn;
+      M = mn;
+    }
+  }
+  return a;
 }
 
 // Output rows: one row's four dims from its maximum, sum and unnormalised mean
+template <int FMT>
 __device__ __forceinline__ void finish_dims(const QAttParams &p, int64_t row, int d4, float4 a, float M, float L) {
-  const float inv = L == 0.f ? 0.f : 1.f / L;   // (0: nothing seen)
+  const float inv = L == 0.f ? 0.f : 1.f / kUnit<FMT> / L;   // (0: nothing seen)
   *reinterpret_cast<uint2 *>(p.out + row * LOCKS_D + d4) = make_uint2(pack_bf16(a.x * inv, a.y * inv), pack_bf16(a.z * inv, a.w * inv));
-  if (p.lse && d4 == 0) p.lse[row] = L == 0.f ? -INFINITY : ((M == -INFINITY ? 0.f : M) + log2f(L)) * kLn2;
+  if (p.lse && d4 == 0) p.lse[row] = L == 0.f ? -INFINITY : ((M == -INFINITY ? 0.f : M) - 15.f + log2f(L)) * kLn2;
 }
 
-// A warp's ring: tiles of 4 KB (keys, then values; 16 rows of 128 bytes).  16-byte pieces of a row are stored at piece ^ 4 (row % 2)
-// (keys) and piece ^ 2 (row / 2 % 4) (values): then the eight lanes that read together, two rows' pieces 4 c .. 4 c + 3 (keys) or four
-// rows' pieces 2 c, 2 c + 1 (values), touch every bank once.
-constexpr int kTile = 2 * 16 * LOCKS_D;
-template <int NH> constexpr int kStages = NH == 1 ? 3 : 6;
-template <int NH> constexpr int kRing = kStages<NH> * kTile;
+// A warp's ring: pairs of tiles; a tile is 4 KB (keys, then values; 16 rows of 128 bytes).  16-byte pieces of a row are stored at piece
+// ^ 4 (row % 2) (keys) and piece ^ 2 (row / 2 % 4) (values): then the eight lanes that read together, two rows' pieces 4 c .. 4 c + 3
+// (keys) or four rows' pieces 2 c, 2 c + 1 (values), touch every bank once.
+constexpr int kTile = 2 * 16 * LOCKS_D, kPair = 2 * kTile;
+template <int NH> constexpr int kStages = NH == 1 ? 2 : 3;
+template <int NH> constexpr int kCtasPerSm = NH == 1 ? 3 : 2;
+template <int NH> constexpr int kRing = kStages<NH> * kPair;
 template <int NH> constexpr int token_smem() { return kWarps * kRing<NH> + 16; }
 static_assert(kRing<1> >= 8 * (kRowPad * 4 + 8) && kRing<2> >= 16 * (kRowPad * 4 + 8), "a warp's partial takes its ring's place");
-template <int NH> constexpr int kCtasPerSm = NH == 1 ? 4 : 2;
 
-template <int NH, int FMT>
+template <int FMT> constexpr float kScaleUnit = FMT == LOCKS_KVQ_INT ? 1.f : kUnit<FMT>;   // (signed codes come in their unit)
+
+// codes of a word (flipped, if signed) as fp16 in units of kUnit (signed) or 1
+template <int FMT> __device__ __forceinline__ void halves(uint32_t w, uint32_t &lo, uint32_t &hi) {
+  if (FMT == LOCKS_KVQ_INT) { lo = __byte_perm(w, 0, 0x4140); hi = __byte_perm(w, 0, 0x4342); }
+  else kvq_halves<LOCKS_KVQ_FLOAT>(w, lo, hi);
+}
+
+template <int NH, int FMT, bool CONTIG>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm<NH>) kvq_token_kernel(const __grid_constant__ QAttParams p) {
   extern __shared__ __align__(128) uint8_t ring_s[];
   constexpr int R = 8 * NH, S = kStages<NH>;
@@ -373,172 +480,234 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<NH>) kvq_token_kernel(con
   int &last_s = *reinterpret_cast<int *>(ring_s + kWarps * kRing<NH>);
   pdl_trigger();
   pdl_wait();
-  const int64_t all = line_length(p, lane);
-  const int64_t share = share_of(all);
-  int64_t u = share * blockIdx.x;
-  const int64_t u_end = min(u + share, all);
-  int b = -1;
-  int64_t begin = 0;
+  Line line;
+  line.read(p, lane);
+  const int share = share_of(line.all, gridDim.x);
+  if ((int64_t)share * blockIdx.x >= line.all) return;
+  int u = share * blockIdx.x, b = -1, begin = 0;
+  const int u_end = min((int64_t)u + share, (int64_t)line.all);
   Request req = {0, 0, 0, 0, 0};
-  // 16-byte copies: copy i moves piece lane & 7 of row (lane >> 3) + 4 i
+  // 16-byte copies: copy i of a tile moves piece lane & 7 of row (lane >> 3) + 4 i
   const int cr = lane >> 3, cc = lane & 7;
   const uint32_t k_dst = cr * 128 + ((cc ^ (4 * (cr & 1))) << 4), v_dst = 2048 + cr * 128 + ((cc ^ (2 * (cr >> 1))) << 4);
-  const int64_t c_off = (int64_t)cr * p.c.st + cc * 16;
+  const int64_t st = CONTIG ? LOCKS_D : p.c.st, c_off = (int64_t)cr * st + cc * 16;
   while (u < u_end) {
-    if (b < 0 || u >= begin + (int64_t)req.tiles * req.row_tiles * p.Hkv)
-      if (!find_request(p, u, lane, b, begin, req)) return;   // (not reached: u lies on the line)
-    const int prob = (int)((u - begin) / req.tiles);            // problem of the request
-    const int64_t prob_begin = begin + (int64_t)prob * req.tiles;
-    const int seg0 = (int)(u - prob_begin), seg1 = (int)min((int64_t)req.tiles, u_end - prob_begin);
+    if (b < 0 || u >= begin + places(p, req)) line.find(p, u, lane, b, begin, req);
+    const int span = kLead + req.pairs, prob = (u - begin) / span, prob_begin = begin + prob * span;   // problem of the request
+    const int seg0 = max(u - prob_begin - kLead, 0), seg1 = min(req.pairs, u_end - prob_begin - kLead);
+    u = prob_begin + kLead + max(seg1, 0);
+    if (seg1 <= seg0) continue;   // (nothing but some of the problem's lead)
     const int h = prob % p.Hkv, rt = prob / p.Hkv, hkv = h / p.kvdiv, kv_heads = p.Hkv / p.kvdiv;
     const int j0 = rt * p.tile_tokens, toks = min(p.tile_tokens, req.n - j0), rows = toks * p.G;
     const int T = req.T, B = p.c.B, full_pages = T > 0 ? T / B : 0;
-    int npages = 0;
+    int tiles = p.c.Pmax << p.sub_shift;   // (a dense problem's further tiles lie behind its tokens)
     if (p.ids) {
-      npages = p.cnt[(int64_t)b * p.Hkv + h];
+      int npages = p.cnt[(int64_t)b * p.Hkv + h];
       if (npages < 0 || npages > p.kbud) {
         if (tid == 0) set_status(p.status, LOCKS_ERR_BAD_BLOCK);
         npages = npages < 0 ? 0 : p.kbud;
       }
+      tiles = npages << p.sub_shift;
     }
-    const int tiles_here = p.ids ? min(seg1, npages << p.sub_shift) : (T > 0 ? seg1 : 0);
-    // ---- the segment's tiles: this warp's are seg0 + warp + 4 j
-    const int first = seg0 + warp, sub_mask = (1 << p.sub_shift) - 1;
-    const int mine = tiles_here > first ? (tiles_here - first + kWarps - 1) / kWarps : 0;
-    // blocks and scales of 32 tiles at a time, a lane each.  block -1: nothing to read here (out of range, past the end); -2: the unfinished page
-    int blk = -1, blk_next = -1, page_l = 0, page_next = 0;
-    float ks_l = 0.f, vs_l = 0.f, ks_next = 0.f, vs_next = 0.f;
-    uint64_t tails = 0;   // times that each 16-token part of the unfinished page is listed, 16 bits a part
-    auto resolve = [&](int jb, int &bk, int &pg, float &ks, float &vs) {
-      const int idx = first + (jb + lane) * kWarps;
-      bk = -1; pg = 0; ks = vs = 0.f;
-      if (idx < tiles_here) {
-        pg = idx >> p.sub_shift;
-        if (p.ids) pg = p.ids[((int64_t)b * p.Hkv + h) * p.kbud + pg];
-        if (pg < 0 || pg >= p.c.Pmax) {
+    const int lim_min = T - req.n + j0 + 1;   // what the row tile's first token sees
+    // ---- the segment's pairs: this warp's are seg0 + warp + 4 j.  Blocks and scales of 16 pairs at a time, a lane per tile.
+    const int first = seg0 + warp, sub_mask = (1 << p.sub_shift) - 1, end = min(seg1, (tiles + 1) >> 1);
+    const int mine = end > first ? (end - first + kWarps - 1) / kWarps : 0;
+    struct Batch {
+      int blk, page;         // block, page of this lane's tile
+      float ks, vs;
+      uint32_t have, easy;   // tiles of codes; those among them that every row sees whole.  Not uniform bits of the others: 0
+    };
+    auto tile_at = [&](int jb) { return 2 * (first + (jb + (lane >> 1)) * kWarps) + (lane & 1); };
+    auto page_at = [&](int tile) { return p.ids ? p.ids[((int64_t)b * p.Hkv + h) * p.kbud + (tile >> p.sub_shift)] : tile >> p.sub_shift; };
+    auto resolve = [&](int jb) {
+      const int tile = tile_at(jb);
+      Batch r = {-1, 0, 0.f, 0.f, 0, 0};
+      if (tile < min(tiles, 2 * end)) {
+        r.page = page_at(tile);
+        if (r.page < 0 || r.page >= p.c.Pmax) {
           set_status(p.status, LOCKS_ERR_BAD_BLOCK);
-        } else if (pg < full_pages) {
-          bk = p.c.block_table[(int64_t)b * p.c.Pmax + pg];
-          if (bk < 0 || bk >= p.c.num_blocks) {
-            bk = -1;
+        } else if (r.page < full_pages) {
+          r.blk = p.c.block_table[(int64_t)b * p.c.Pmax + r.page];
+          if (r.blk < 0 || r.blk >= p.c.num_blocks) {
+            r.blk = -1;
             set_status(p.status, LOCKS_ERR_BAD_BLOCK);
           } else {
-            const int64_t at = (int64_t)bk * kv_heads + hkv;
-            ks = p.c.ks[at];
-            vs = p.c.vs[at];
+            const int64_t at = (int64_t)r.blk * kv_heads + hkv;
+            r.ks = p.c.ks[at];
+            r.vs = p.c.vs[at];
           }
-        } else if (pg == full_pages && pg * B + (idx & sub_mask) * 16 < T) {
-          bk = -2;
+        } else if (r.page == full_pages && r.page * B + (tile & sub_mask) * 16 < T) {
+          r.blk = kUnfinished;
         }
       }
+      __syncwarp();
+      r.have = __ballot_sync(0xffffffffu, r.blk >= 0);
+      r.easy = __ballot_sync(0xffffffffu, r.blk >= 0 && r.page * B + (tile & sub_mask) * 16 + 16 <= lim_min);
+      return r;
     };
-    resolve(0, blk, page_l, ks_l, vs_l);
-    auto sub_of = [&](int j) { return (first + j * kWarps) & sub_mask; };
-    auto issue = [&](int j, int bk) {
-      if (j < mine && bk >= 0) {
-        uint8_t *dst = ring + (j % S) * kTile;
-        const int64_t off = (int64_t)bk * p.c.sb + (int64_t)hkv * p.c.sh + (int64_t)(sub_of(j) * 16) * p.c.st + c_off;
-        const char *kp = p.c.k + off, *vp = p.c.v + off;
+    Batch cur = resolve(0), next = cur;
+    auto issue = [&](int j, const Batch &r) {   // a pair's copies
+      uint8_t *dst = ring + (j % S) * kPair;
+      const int l = 2 * (j & 15);
+      if (j < mine) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          copy16(dst + k_dst + 512 * i, kp + 4 * i * p.c.st);
-          copy16(dst + (v_dst ^ (64 * (i & 1))) + 512 * i, vp + 4 * i * p.c.st);
+        for (int w = 0; w < 2; ++w) {
+          const int bk = __shfl_sync(0xffffffffu, r.blk, l + w);
+          if ((r.have >> (l + w)) & 1) {
+            const int sub = (2 * (first + j * kWarps) + w) & sub_mask;
+            const int64_t off = (int64_t)bk * p.c.sb + (int64_t)hkv * p.c.sh + (int64_t)(sub * 16) * st + c_off;
+            const char *kp = p.c.k + off, *vp = p.c.v + off;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              copy16(dst + w * kTile + k_dst + 512 * i, kp + 4 * i * st);
+              copy16(dst + w * kTile + (v_dst ^ (64 * (i & 1))) + 512 * i, vp + 4 * i * st);
+            }
+          }
         }
       }
       cp_async_commit();
     };
 #pragma unroll
-    for (int j = 0; j < S - 1; ++j) issue(j, __shfl_sync(0xffffffffu, blk, j));
+    for (int j = 0; j < S - 1; ++j) issue(j, cur);
     uint32_t qf[NH][8][2];
-    float rs[NH];   // 2^e of the row, times sm_scale log2 e
-    load_queries<NH>(p, req.row0 + j0, h, rows, x, t, qf, rs);
+    float rs[NH], start[NH];
+    load_queries<NH>(p, req.row0 + j0, h, rows, x, t, qf, rs, start);
     int lim[NH];    // row x (+ 8) sees the first lim tokens
 #pragma unroll
     for (int hh = 0; hh < NH; ++hh) lim[hh] = x + 8 * hh < rows ? T - req.n + j0 + (x + 8 * hh) / p.G + 1 : T;
-    const int lim_min = T - req.n + j0 + 1;   // what the tile's first token sees
     Running<NH> run;
     run.clear();
-#pragma unroll 1
-    for (int j = 0; j < mine; ++j) {
-      const int jn = j + S - 1;
-      if ((jn & 31) == 16) resolve(jn + 16, blk_next, page_next, ks_next, vs_next);   // half a batch early
-      const bool over = (jn & 31) < S - 1 && jn >= 32;   // tile j + S - 1 is of the next batch, tile j of this one
-      issue(jn, __shfl_sync(0xffffffffu, over ? blk_next : blk, jn & 31));
-      cp_async_wait<S - 1>();
-      __syncwarp();
-      const int bk = __shfl_sync(0xffffffffu, blk, j & 31), pos = __shfl_sync(0xffffffffu, page_l, j & 31) * B + sub_of(j) * 16;
-      const float ks = __shfl_sync(0xffffffffu, ks_l, j & 31), vs = __shfl_sync(0xffffffffu, vs_l, j & 31);
-      if (bk == -2) tails += 1ull << (16 * sub_of(j));
-      if (bk >= 0) {
-        const uint8_t *kt = ring + (j % S) * kTile, *vt = kt + 2048;
-        float s[2][4];
 #pragma unroll
-        for (int w = 0; w < 2; ++w) {
+    for (int hh = 0; hh < NH; ++hh) {
+      if (FMT == LOCKS_KVQ_INT) rs[hh] *= 0x1p24f;
+      else start[hh] = 0.f;
+    }
+    // scores of a tile: two chains of four steps for each eight tokens
+    auto scores = [&](const uint8_t *kt, float (&s)[2][4]) {
 #pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            const uint4 y = *reinterpret_cast<const uint4 *>(kt + (x + 8 * w) * 128 + (((4 * c + t) ^ (4 * (x & 1))) << 4));
-            const uint32_t word[4] = {y.x, y.y, y.z, y.w};
+      for (int w = 0; w < 2; ++w) {
+        float c[2][4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int st = 4 * c + i;
-              uint32_t lo, hi;
-              kvq_halves<FMT>(kvq_flip<FMT>(word[i]), lo, hi);
-              if (st == 0) mma_f16_z(s[w], qf[0][st][0], NH == 2 ? qf[NH - 1][st][0] : 0u, qf[0][st][1], NH == 2 ? qf[NH - 1][st][1] : 0u, lo, hi);
-              else mma_f16(s[w], qf[0][st][0], NH == 2 ? qf[NH - 1][st][0] : 0u, qf[0][st][1], NH == 2 ? qf[NH - 1][st][1] : 0u, lo, hi);
-            }
+        for (int half = 0; half < 2; ++half) {
+          const uint4 y = *reinterpret_cast<const uint4 *>(kt + (x + 8 * w) * 128 + (((4 * half + t) ^ (4 * (x & 1))) << 4));
+          const uint32_t word[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int k = 4 * half + i;
+            uint32_t lo, hi;
+            halves<FMT>(kvq_flip<FMT>(word[i]), lo, hi);
+            const uint32_t a1 = NH == 2 ? qf[NH - 1][k][0] : 0u, a3 = NH == 2 ? qf[NH - 1][k][1] : 0u;
+            if (k == 0) mma_f16_from(c[0], qf[0][k][0], a1, qf[0][k][1], a3, lo, hi, start[0], start[0], start[NH - 1], start[NH - 1]);
+            else if (k == 4) mma_f16_from(c[1], qf[0][k][0], a1, qf[0][k][1], a3, lo, hi, 0.f, 0.f, 0.f, 0.f);
+            else mma_f16(c[half], qf[0][k][0], a1, qf[0][k][1], a3, lo, hi);
           }
         }
-        uint32_t pb[NH][2];
-        float pw[NH][4], f[NH];
-        float2 fv[NH];
 #pragma unroll
-        for (int hh = 0; hh < NH; ++hh) { f[hh] = rs[hh] * ks; fv[hh] = make_float2(vs, vs); }
-        const bool mask = pos + 16 > lim_min;
-        run.weights(s, f, lim, pos, mask, t, pb, pw);
-        if (mask) {   // rows that see nothing of the tile take nothing of it, not even a NaN that its scale may be
+        for (int e = 0; e < 4; ++e) s[w][e] = c[0][e] + c[1][e];
+      }
+    };
+    auto values = [&](const uint8_t *vt, const uint32_t (&pb)[NH][2], const float2 (&fv)[NH]) {
+      float2 from[NH];
 #pragma unroll
-          for (int hh = 0; hh < NH; ++hh) {
-            if (pos >= __shfl_sync(0xffffffffu, lim[hh], 8 * t)) fv[hh].x = 0.f;
-            if (pos >= __shfl_sync(0xffffffffu, lim[hh], 8 * t + 4)) fv[hh].y = 0.f;
-          }
-        }
-        uint4 v[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int tok = 2 * t + (e & 1) + 4 * (e & 2);
-          v[e] = *reinterpret_cast<const uint4 *>(vt + tok * 128 + ((x ^ (2 * t)) << 4));
-        }
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          auto word = [&](int e) { return kvq_flip<FMT>(w == 0 ? v[e].x : (w == 1 ? v[e].y : (w == 2 ? v[e].z : v[e].w))); };
-          const uint32_t a0 = word(0), a1 = word(1), a2 = word(2), a3 = word(3);
-          uint32_t ha[4][2];   // [dim][token pair]
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            const uint32_t lo = c ? a2 : a0, hi = c ? a3 : a1;
-            kvq_halves<FMT>(__byte_perm(lo, hi, 0x5140), ha[0][c], ha[1][c]);
-            kvq_halves<FMT>(__byte_perm(lo, hi, 0x7362), ha[2][c], ha[3][c]);
-          }
-          run.outputs(2 * w, ha[0][0], ha[1][0], ha[0][1], ha[1][1], pb, fv);
-          run.outputs(2 * w + 1, ha[2][0], ha[3][0], ha[2][1], ha[3][1], pb, fv);
+      for (int hh = 0; hh < NH; ++hh) {
+        from[hh] = make_float2(0.f, 0.f);
+        if (FMT == LOCKS_KVQ_INT) {   // 128 sum of weights
+          float c[4];
+          mma_f16_from(c, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u, pb[hh][0], pb[hh][1], 0.f, 0.f, 0.f, 0.f);
+          from[hh] = make_float2(-0x1p-17f * c[0], -0x1p-17f * c[1]);
         }
       }
-      if ((j & 31) == 31) { blk = blk_next; page_l = page_next; ks_l = ks_next; vs_l = vs_next; }
+      uint4 v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = *reinterpret_cast<const uint4 *>(vt + (2 * t + (e & 1) + 4 * (e & 2)) * 128 + ((x ^ (2 * t)) << 4));
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        auto word = [&](int e) { return kvq_flip<FMT>(w == 0 ? v[e].x : (w == 1 ? v[e].y : (w == 2 ? v[e].z : v[e].w))); };
+        const uint32_t a0 = word(0), a1 = word(1), a2 = word(2), a3 = word(3);
+        uint32_t ha[4][2];   // [dim][token pair]
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const uint32_t lo = c ? a2 : a0, hi = c ? a3 : a1;
+          halves<FMT>(__byte_perm(lo, hi, 0x5140), ha[0][c], ha[1][c]);
+          halves<FMT>(__byte_perm(lo, hi, 0x7362), ha[2][c], ha[3][c]);
+        }
+        run.outputs(2 * w, ha[0][0], ha[1][0], ha[0][1], ha[1][1], pb, from, fv);
+        run.outputs(2 * w + 1, ha[2][0], ha[3][0], ha[2][1], ha[3][1], pb, from, fv);
+      }
+    };
+    uint64_t tails = 0;   // times that each 16-token part of the unfinished page is listed, 16 bits a part
+#pragma unroll 1
+    for (int j = 0; j < mine; ++j) {
+      const int jn = j + S - 1, l = 2 * (j & 15);
+      if ((jn & 15) == 8) next = resolve((jn & ~15) + 16);   // half a batch early
+      if ((jn & 15) < S - 1 && jn >= 16) issue(jn, next);    // (pair j + S - 1 is of the next batch, pair j of this one)
+      else issue(jn, cur);
+      cp_async_wait<S - 1>();
+      __syncwarp();
+      const uint8_t *pair = ring + (j % S) * kPair;
+      const float ks[2] = {__shfl_sync(0xffffffffu, cur.ks, l), __shfl_sync(0xffffffffu, cur.ks, l + 1)};
+      const float vs[2] = {__shfl_sync(0xffffffffu, cur.vs, l) * kScaleUnit<FMT>, __shfl_sync(0xffffffffu, cur.vs, l + 1) * kScaleUnit<FMT>};
+      if (((cur.easy >> l) & 3) == 3) {
+        float s[4][4], f[2][NH], pw[2][NH][4];
+        uint32_t pb[2][NH][2];
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          float sw[2][4];
+          scores(pair + w * kTile, sw);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) { s[2 * w][e] = sw[0][e]; s[2 * w + 1][e] = sw[1][e]; }
+#pragma unroll
+          for (int hh = 0; hh < NH; ++hh) f[w][hh] = rs[hh] * ks[w];
+        }
+        run.template weights<2, false>(s, f, lim, 0, t, pb, pw);
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          float2 fv[NH];
+#pragma unroll
+          for (int hh = 0; hh < NH; ++hh) fv[hh] = make_float2(vs[w], vs[w]);
+          values(pair + w * kTile + 2048, pb[w], fv);
+        }
+      } else {
+#pragma unroll 1
+        for (int w = 0; w < 2; ++w) {
+          const int sub = (2 * (first + j * kWarps) + w) & sub_mask;
+          const int pos = __shfl_sync(0xffffffffu, cur.page, l + w) * B + sub * 16;
+          if (!((cur.have >> (l + w)) & 1)) {
+            if (__shfl_sync(0xffffffffu, cur.blk, l + w) == kUnfinished) tails += 1ull << (16 * sub);
+            continue;
+          }
+          float s[2][4], f[1][NH], pw[1][NH][4];
+          uint32_t pb[1][NH][2];
+          float2 fv[NH];
+          scores(pair + w * kTile, s);
+#pragma unroll
+          for (int hh = 0; hh < NH; ++hh) {   // rows that see nothing of the tile take nothing of it, not even a NaN that its scale may be
+            f[0][hh] = rs[hh] * (w ? ks[1] : ks[0]);
+            fv[hh].x = pos < __shfl_sync(0xffffffffu, lim[hh], 8 * t) ? (w ? vs[1] : vs[0]) : 0.f;
+            fv[hh].y = pos < __shfl_sync(0xffffffffu, lim[hh], 8 * t + 4) ? (w ? vs[1] : vs[0]) : 0.f;
+          }
+          run.template weights<1, true>(s, f, lim, pos, t, pb, pw);
+          values(pair + w * kTile + 2048, pb[0], fv);
+        }
+      }
+      if ((j & 15) == 15) cur = next;
       __syncwarp();
     }
     // ---- the warps' partials
     cp_async_wait<0>();
     __syncwarp();
-    run.leave(part_of(warp), ml_of(warp), x, t, false, 1.f);
+    run.template leave<false>(part_of(warp), ml_of(warp), x, t, 1.f);
     __syncwarp();
+#pragma unroll 1
     for (int sub = 0; tails; ++sub, tails >>= 16) {
       if (!(tails & 0xffff)) continue;
       const int64_t at = (((int64_t)b * kv_heads + hkv) * B + 16 * sub) * LOCKS_D;
-      tail_tile<NH>(p, req.row0 + j0, h, rows, T, lim, p.c.kt + at, p.c.vt + at, full_pages * B + 16 * sub, (float)(tails & 0xffff), part_of(warp), ml_of(warp));
+      tail_tile<NH, FMT>(p, req.row0 + j0, h, rows, T, lim[0], lim[NH - 1], p.c.kt + at, p.c.vt + at, full_pages * B + 16 * sub, (float)(tails & 0xffff), part_of(warp), ml_of(warp));
       __syncwarp();
     }
     __syncthreads();
-    const bool whole = seg0 == 0 && seg1 == req.tiles;
+    const bool whole = seg0 == 0 && seg1 == req.pairs;
     const int slot = 2 * blockIdx.x + (seg0 == 0 ? 1 : 0);
     auto row_of = [&](int r) { const int j = r / p.G; return (int64_t)(req.row0 + j0 + j) * p.Hq + h * p.G + (r - j * p.G); };
     for (int i = tid; i < rows * (LOCKS_D / 4); i += kThreads) {
@@ -556,41 +725,84 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<NH>) kvq_token_kernel(con
         a.x = fmaf(y.x, f, a.x); a.y = fmaf(y.y, f, a.y); a.z = fmaf(y.z, f, a.z); a.w = fmaf(y.w, f, a.w);
       }
       if (whole) {
-        finish_dims(p, row_of(r), d4, a, M, L);
+        finish_dims<FMT>(p, row_of(r), d4, a, M, L);
       } else {
         __stcg(reinterpret_cast<float4 *>(p.part + ((int64_t)slot * KVQ_ROWS + r) * LOCKS_D + d4), a);
         if (d4 == 0) __stcg(p.part_ml + slot * KVQ_ROWS + r, make_float2(M, L));
       }
     }
-    if (!whole) {   // the last of the problem's CTAs puts its partials together, in their order
-      const int c0 = (int)(prob_begin / share), c1 = (int)((prob_begin + req.tiles - 1) / share);
-      __threadfence();
+    if (!whole && p.done) {   // the last of the problem's CTAs puts its partials together, in their order
+      const int c0 = (prob_begin + kLead) / share, c1 = (prob_begin + kLead + req.pairs - 1) / share;
       __syncthreads();
-      if (tid == 0) last_s = atomicAdd(p.done + c0, 1) == c1 - c0;
+      if (tid == 0) {
+        __threadfence();   // what the CTA has written, which the barrier orders before
+        last_s = atomicAdd(p.done + c0, 1) == c1 - c0;
+        __threadfence();
+      }
       __syncthreads();
       if (last_s) {
-        __threadfence();
         for (int i = tid; i < rows * (LOCKS_D / 4); i += kThreads) {
           const int r = i >> 5, d4 = 4 * (i & 31);
-          float M = -INFINITY, L = 0.f;
-          float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-          for (int c = c0; c <= c1; ++c) {
-            const int s = 2 * c + (c == c0 ? 1 : 0);
-            const float2 ml = __ldcg(p.part_ml + s * KVQ_ROWS + r);
-            const float4 y = __ldcg(reinterpret_cast<const float4 *>(p.part + ((int64_t)s * KVQ_ROWS + r) * LOCKS_D + d4));
-            const float mn = fmaxf(M, ml.x), fo = mn == -INFINITY ? 1.f : ex2f(M - mn), fn = mn == -INFINITY ? 1.f : ex2f(ml.x - mn);
-            L = L * fo + ml.y * fn;
-            a.x = a.x * fo + y.x * fn; a.y = a.y * fo + y.y * fn; a.z = a.z * fo + y.z * fn; a.w = a.w * fo + y.w * fn;
-            M = mn;
-          }
-          finish_dims(p, row_of(r), d4, a, M, L);
+          float M, L;
+          const float4 a = join_partials(p, c0, c0, c1, 1, r, d4, M, L);
+          finish_dims<FMT>(p, row_of(r), d4, a, M, L);
         }
         if (tid == 0) p.done[c0] = 0;   // ready for the next launch
       }
     }
     __syncthreads();   // the partials' memory is the rings'
-    u = prob_begin + seg1;
   }
+}
+
+// Problems that many CTAs share: a CTA per output row puts their partials together, a warp every fourth of them.
+template <int FMT>
+__global__ void __launch_bounds__(kThreads) kvq_join_kernel(const __grid_constant__ QAttParams p, int ctas) {
+  __shared__ float4 a_s[kWarps][32];
+  __shared__ float2 ml_s[kWarps];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int hq = blockIdx.x, row = blockIdx.y, h = hq / p.G;
+  pdl_trigger();
+  pdl_wait();
+  // the row's request (all warps alike), and where its part of the line begins
+  int b = p.cu ? -1 : row;
+  for (int b0 = 0; p.cu && b0 < p.batch; b0 += 32) {
+    const uint32_t has = __ballot_sync(0xffffffffu, b0 + lane < p.batch && p.cu[b0 + lane] <= row && row < p.cu[b0 + lane + 1]);
+    if (has) { b = b0 + __ffs(has) - 1; break; }
+  }
+  if (b < 0) return;
+  const Request req = request_at(p, b);
+  const int j = row - req.row0;
+  if (j >= req.n) return;   // (offsets out of range)
+  Line line;
+  line.read(p, lane);
+  const int share = share_of(line.all, ctas);
+  int before = 0;   // places of the requests before
+  if (b < 32) {
+    before = __shfl_sync(0xffffffffu, line.end - places(p, line.r), b);
+  } else {
+    before = __shfl_sync(0xffffffffu, line.end, 31);
+    for (int b0 = 32; b0 < b; b0 += 32) before += __reduce_add_sync(0xffffffffu, b0 + lane < b ? places(p, request_at(p, b0 + lane)) : 0);
+  }
+  const int rt = j / p.tile_tokens, r = (j - rt * p.tile_tokens) * p.G + hq - h * p.G;
+  const int at = before + (rt * p.Hkv + h) * (kLead + req.pairs) + kLead;   // its first pair
+  const int c0 = at / share, c1 = (at + req.pairs - 1) / share;
+  if (c0 == c1) return;     // finished by its CTA
+  float M, L;
+  const float4 a = join_partials(p, c0, c0 + warp, c1, kWarps, r, 4 * lane, M, L);
+  a_s[warp][lane] = a;
+  if (lane == 0) ml_s[warp] = make_float2(M, L);
+  __syncthreads();
+  if (warp) return;
+  M = -INFINITY; L = 0.f;
+  for (int w = 0; w < kWarps; ++w) M = fmaxf(M, ml_s[w].x);
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int w = 0; w < kWarps; ++w) {
+    const float f = M == -INFINITY ? 1.f : ex2f(ml_s[w].x - M);
+    const float4 y = a_s[w][lane];
+    L += ml_s[w].y * f;
+    o.x = fmaf(y.x, f, o.x); o.y = fmaf(y.y, f, o.y); o.z = fmaf(y.z, f, o.z); o.w = fmaf(y.w, f, o.w);
+  }
+  finish_dims<FMT>(p, (int64_t)row * p.Hq + hq, 4 * lane, o, M, L);
 }
 
 }  // namespace
@@ -614,17 +826,31 @@ extern "C" int locks_kvq_attend(locks_ctx *ctx, const void *q, const int32_t *cu
   p.tile_tokens = (wide ? 16 : 8) / p.G;
   int ctas = ctx->num_sms * (wide ? kCtasPerSm<2> : kCtasPerSm<1>);
   if (ctas > KVQ_SLOT_BOUND) ctas = KVQ_SLOT_BOUND;
+  // Few problems, each shared by many CTAs: a kernel of its own puts the partials together, row by row, side by side
+  const int64_t problems = (cu_tokens ? std::max<int64_t>(batch, num_tokens / p.tile_tokens) : batch) * p.Hkv;
+  const bool join = ctas >= kManyShares * problems;
+  if (join) p.done = nullptr;
+  const bool contig = kv->stride_token == LOCKS_D;
   ctx->last_launches = 0;
-#define KVQ_TOKEN(NH_, F_)                                                                                                            \
+#define KVQ_TOKEN(NH_, F_, C_)                                                                                                        \
   do {                                                                                                                                \
-    if (locks_attrs_needed(LOCKS_ATTR_KVQ + 2 * (NH_ - 1) + F_))                                                                      \
-      cudaFuncSetAttribute(kvq_token_kernel<NH_, F_>, cudaFuncAttributeMaxDynamicSharedMemorySize, token_smem<NH_>());                \
-    locks_launch_pdl(kvq_token_kernel<NH_, F_>, dim3(ctas), dim3(kThreads), token_smem<NH_>(), (cudaStream_t)stream, p);              \
+    if (wide != (NH_ == 2) || kv->fmt != F_ || contig != C_) break;                                                                   \
+    if (locks_attrs_needed(LOCKS_ATTR_KVQ + 4 * (NH_ - 1) + 2 * F_ + C_))                                                             \
+      cudaFuncSetAttribute(kvq_token_kernel<NH_, F_, C_>, cudaFuncAttributeMaxDynamicSharedMemorySize, token_smem<NH_>());            \
+    locks_launch_pdl(kvq_token_kernel<NH_, F_, C_>, dim3(ctas), dim3(kThreads), token_smem<NH_>(), (cudaStream_t)stream, p);          \
   } while (0)
-  if (!wide && kv->fmt == LOCKS_KVQ_INT) KVQ_TOKEN(1, LOCKS_KVQ_INT);
-  else if (!wide) KVQ_TOKEN(1, LOCKS_KVQ_FLOAT);
-  else if (kv->fmt == LOCKS_KVQ_INT) KVQ_TOKEN(2, LOCKS_KVQ_INT);
-  else KVQ_TOKEN(2, LOCKS_KVQ_FLOAT);
+  KVQ_TOKEN(1, LOCKS_KVQ_INT, true);
+  KVQ_TOKEN(1, LOCKS_KVQ_INT, false);
+  KVQ_TOKEN(1, LOCKS_KVQ_FLOAT, true);
+  KVQ_TOKEN(1, LOCKS_KVQ_FLOAT, false);
+  KVQ_TOKEN(2, LOCKS_KVQ_INT, true);
+  KVQ_TOKEN(2, LOCKS_KVQ_INT, false);
+  KVQ_TOKEN(2, LOCKS_KVQ_FLOAT, true);
+  KVQ_TOKEN(2, LOCKS_KVQ_FLOAT, false);
 #undef KVQ_TOKEN
+  if ((rc = locks_check_launch(ctx)) != LOCKS_OK || !join) return rc;
+  const dim3 rows(p.Hq, num_tokens);
+  if (kv->fmt == LOCKS_KVQ_INT) locks_launch_pdl(kvq_join_kernel<LOCKS_KVQ_INT>, rows, dim3(kThreads), 0, (cudaStream_t)stream, p, ctas);
+  else locks_launch_pdl(kvq_join_kernel<LOCKS_KVQ_FLOAT>, rows, dim3(kThreads), 0, (cudaStream_t)stream, p, ctas);
   return locks_check_launch(ctx);
 }
