@@ -27,9 +27,10 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kRowPad = LOCKS_D + 4;   // floats of a row of a warp's partial
 constexpr int kUnfinished = -2;        // in a block's place: the unfinished page
+constexpr int kMostLead = 24;          // pairs that a problem's start costs a CTA that has another one's end before it
+constexpr int kMinShare = kWarps;      // places of a share at least: a pair per warp
+constexpr int kJoinWarps = 8;
 constexpr int kManyShares = 16;        // CTAs per problem from which on the partials are put together by a second kernel
-constexpr int kLead = 6;               // what a problem's start costs, in pairs: so many places of the line come before its pairs
-constexpr int kMinShare = kLead + kWarps;      // pairs of tiles of a share at least: one per warp
 
 struct QAttParams {
   const __nv_bfloat16 *q;
@@ -92,8 +93,6 @@ __device__ __forceinline__ Request request_at(const QAttParams &p, int b) {
   return r;
 }
 
-__device__ __forceinline__ int places(const QAttParams &p, const Request &r) { return (kLead + r.pairs) * r.row_tiles * p.Hkv; }
-
 // 32 requests, a lane each: where their places end within the 32; the warp's total in lane 31
 __device__ __forceinline__ int scan_places(int mine, int lane) {
 #pragma unroll
@@ -104,20 +103,29 @@ __device__ __forceinline__ int scan_places(int mine, int lane) {
   return mine;
 }
 
-// What a warp knows of the line: the first 32 requests (most batches: all), and the line's length.  (The host sees to it that the
-// length fits 32 bits.)
+// The line as a warp knows it: the first 32 requests (most batches: all), its length and the CTAs' share of it.  (The host sees to it
+// that the length fits 32 bits.)  A problem's pairs come after `lead` places that stand for what its start costs: its queries, first
+// blocks and tiles, and joining its warps' partials take a CTA some 10 us, as long as 24 pairs do.  Without them a CTA with two
+// problems in its share ends that much later (24 requests of 211 .. 9001 tokens, 8 heads: 76 us; 6 places 66, 24 places 51).  A quarter of
+// the share at most: where shares are short every CTA has a start of its own, and places without work would leave CTAs idle.
 struct Line {
-  Request r;        // lane: request
-  int end, all;     // lane: the end of its places
-  __device__ __forceinline__ void read(const QAttParams &p, int lane) {
+  Request r;                   // lane: request
+  int end, all, lead, share;   // end: of the lane's request's places
+  __device__ __forceinline__ int places(const QAttParams &p, const Request &x) const { return (lead + x.pairs) * x.row_tiles * p.Hkv; }
+  __device__ __forceinline__ void read(const QAttParams &p, int lane, int ctas) {
     r = Request{0, 0, 0, 0, 0};
     if (lane < p.batch) r = request_at(p, lane);
-    end = scan_places(places(p, r), lane);
-    all = __shfl_sync(0xffffffffu, end, 31);
+    int pairs = __reduce_add_sync(0xffffffffu, r.pairs * r.row_tiles), problems = __reduce_add_sync(0xffffffffu, r.row_tiles);
     for (int b0 = 32; b0 < p.batch; b0 += 32) {
-      const int mine = b0 + lane < p.batch ? places(p, request_at(p, b0 + lane)) : 0;
-      all += __reduce_add_sync(0xffffffffu, mine);
+      Request x = {0, 0, 0, 0, 0};
+      if (b0 + lane < p.batch) x = request_at(p, b0 + lane);
+      pairs += __reduce_add_sync(0xffffffffu, x.pairs * x.row_tiles);
+      problems += __reduce_add_sync(0xffffffffu, x.row_tiles);
     }
+    lead = min(pairs * p.Hkv / (4 * ctas), kMostLead);
+    all = (pairs + lead * problems) * p.Hkv;
+    share = max((all - 1) / ctas + 1, kMinShare);
+    end = scan_places(places(p, r), lane);
   }
   // The request that holds place u (below `all`), and where its places begin
   __device__ __forceinline__ void find(const QAttParams &p, int u, int lane, int &b, int &begin, Request &req) const {
@@ -141,8 +149,6 @@ struct Line {
     req.pairs = __shfl_sync(0xffffffffu, x.pairs, l); req.row_tiles = __shfl_sync(0xffffffffu, x.row_tiles, l);
   }
 };
-__device__ __forceinline__ int share_of(int all, int ctas) { return max((all - 1) / ctas + 1, kMinShare); }
-
 // Outputs are kept times 2^15 (of the weights) and this: the unit of signed codes' fp16 form; for e4m3, so that large scales stay in range
 template <int FMT> constexpr float kUnit = FMT == LOCKS_KVQ_INT ? 0x1p-24f : 0x1p-15f;
 
@@ -156,19 +162,24 @@ __device__ __forceinline__ float finite_abs(float x) {
   return a < INFINITY ? a : 0.f;
 }
 
-// The row tile's queries as A fragments: lane (x, t) holds four dims of row x (+ 8) per step, 64 (s / 4) + 16 t + 4 (s % 4) ..
-// rs: what undoes the power of two, times c2; start: what signed codes' 128 adds to a row's sum of products, taken off.
+// The row tile's queries as B fragments: lane (x, t) holds four dims of row x (+ 8) per step, 64 (s / 4) + 16 t + 4 (s % 4) ..
+// Of rows 2 t, 2 t + 1 (+ 8), rs: what undoes their power of two, times c2; start: what signed codes' 128 adds to the sum of products,
+// taken off.
 template <int NH>
-__device__ __forceinline__ void load_queries(const QAttParams &p, int64_t row0, int h, int rows, int x, int t, uint32_t (&qf)[NH][8][2], float (&rs)[NH], float (&start)[NH]) {
+__device__ __forceinline__ void fetch_queries(const QAttParams &p, int64_t row0, int h, int rows, int x, int t, uint4 (&w)[NH][4]) {
 #pragma unroll
   for (int hh = 0; hh < NH; ++hh) {
     const int r = x + 8 * hh, j = r / p.G, g = r - j * p.G;
     const __nv_bfloat16 *qr = p.q + ((row0 + j) * p.Hq + h * p.G + g) * LOCKS_D + 16 * t;
-    uint4 w[4] = {};
-    if (r < rows) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const uint4 *>(qr + (i >> 1) * 64 + 8 * (i & 1));
-    }
+    for (int i = 0; i < 4; ++i) w[hh][i] = r < rows ? *reinterpret_cast<const uint4 *>(qr + (i >> 1) * 64 + 8 * (i & 1)) : make_uint4(0, 0, 0, 0);
+  }
+}
+template <int NH>
+__device__ __forceinline__ void take_queries(const QAttParams &p, const uint4 (&raw)[NH][4], int t, uint32_t (&qf)[NH][8][2], float2 (&rs)[NH], float2 (&start)[NH]) {
+#pragma unroll
+  for (int hh = 0; hh < NH; ++hh) {
+    const uint4 (&w)[4] = raw[hh];
     float amax = 0.f;
     float v[8][4];
 #pragma unroll
@@ -187,7 +198,8 @@ __device__ __forceinline__ void load_queries(const QAttParams &p, int64_t row0, 
     amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
     amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
     const float up = power_to(amax, 0);
-    rs[hh] = p.c2 / up;
+    const float back = p.c2 / up;
+    rs[hh] = make_float2(__shfl_sync(0xffffffffu, back, 8 * t), __shfl_sync(0xffffffffu, back, 8 * t + 4));
     float sum = 0.f;
 #pragma unroll
     for (int s = 0; s < 8; ++s)
@@ -195,7 +207,8 @@ __device__ __forceinline__ void load_queries(const QAttParams &p, int64_t row0, 
       for (int e = 0; e < 4; ++e) sum += v[s][e] * up;
     sum += __shfl_xor_sync(0xffffffffu, sum, 1);
     sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-    start[hh] = -0x1p-17f * sum;
+    sum *= -0x1p-17f;
+    start[hh] = make_float2(__shfl_sync(0xffffffffu, sum, 8 * t), __shfl_sync(0xffffffffu, sum, 8 * t + 4));
 #pragma unroll
     for (int s = 0; s < 8; ++s) { qf[hh][s][0] = pack_f16(v[s][0] * up, v[s][1] * up); qf[hh][s][1] = pack_f16(v[s][2] * up, v[s][3] * up); }
   }
@@ -208,61 +221,88 @@ __device__ __forceinline__ void mma_f16_from(float (&d)[4], uint32_t a0, uint32_
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
 }
 
-// Running softmax of the row tile in a warp's registers
+// transpose of an 8 x 8 matrix of 16-bit elements, lane (x, t) holding elements 2 t, 2 t + 1 of row x
+__device__ __forceinline__ uint32_t movm_trans(uint32_t v) {
+  uint32_t d;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
+  return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("mul.rn.f32x2 %0, %1, %2;"
+      : "=l"(*reinterpret_cast<unsigned long long *>(&d))
+      : "l"(*reinterpret_cast<unsigned long long *>(&a)), "l"(*reinterpret_cast<unsigned long long *>(&b)));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("add.rn.f32x2 %0, %1, %2;"
+      : "=l"(*reinterpret_cast<unsigned long long *>(&d))
+      : "l"(*reinterpret_cast<unsigned long long *>(&a)), "l"(*reinterpret_cast<unsigned long long *>(&b)));
+  return d;
+}
+__device__ __forceinline__ float2 max2(float2 a, float2 b) { return make_float2(fmaxf(a.x, b.x), fmaxf(a.y, b.y)); }
+
+// Running softmax of the row tile in a warp's registers, of rows 2 t, 2 t + 1 (+ 8) in every lane
 template <int NH>
 struct Running {
-  float m[NH], l[NH];   // row x (+ 8): maximum (log2 units), this lane's share of the sum
-  float4 o[8][NH];      // dims 16 x + 2 i (.x, .y) and 16 x + 2 i + 1 (.z, .w) of rows 2 t, 2 t + 1 (+ 8)
+  float2 m[NH], l[NH];   // maximum (log2 units); the share of the sum of this lane's tokens
+  float4 o[8][NH];       // dims 16 x + 2 i (.x, .y) and 16 x + 2 i + 1 (.z, .w)
   __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int hh = 0; hh < NH; ++hh) {
-      m[hh] = -INFINITY;
-      l[hh] = 0.f;
+      m[hh] = make_float2(-INFINITY, -INFINITY);
+      l[hh] = make_float2(0.f, 0.f);
 #pragma unroll
       for (int i = 0; i < 8; ++i) o[i][hh] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
   }
-  // Scores of H tiles (of tokens 2 t, 2 t + 1, 8 + 2 t, 9 + 2 t of each) -> weights times 2^15 (pw; as B fragments pb).  f: what the
-  // sums of products stand for, in log2 units.  mask: some row does not see all of the tile, whose first token's place is pos
+  // Scores of H tiles (tokens x and x + 8 of each, by the two rows) -> weights times 2^15 (pw; as B fragments pb).  f: what the sums of
+  // products stand for, in log2 units.  MASK: some row does not see all of the tile, whose first token's place is pos
   template <int H, bool MASK>
-  __device__ __forceinline__ void weights(const float (&s)[2 * H][4], const float (&f)[H][NH], const int (&lim)[NH], int pos, int t, uint32_t (&pb)[H][NH][2], float (&pw)[H][NH][4]) {
+  __device__ __forceinline__ void weights(const float (&s)[H][NH][4], const float2 (&f)[H][NH], const int2 (&lim)[NH], int pos, int x, uint32_t (&pb)[H][NH][2], float (&pw)[H][NH][4]) {
 #pragma unroll
     for (int hh = 0; hh < NH; ++hh) {
-      float sv[H][4];
-#pragma unroll
-      for (int w = 0; w < H; ++w)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          sv[w][e] = s[2 * w + (e >> 1)][2 * hh + (e & 1)];
-          if (MASK) sv[w][e] = pos + 2 * t + (e & 1) + 4 * (e & 2) >= lim[hh] ? -INFINITY : sv[w][e] * f[w][hh];
-        }
-      float mx = -INFINITY;
+      float2 v[H][2], mx = make_float2(-INFINITY, -INFINITY);
 #pragma unroll
       for (int w = 0; w < H; ++w) {
-        const float m4 = fmaxf(fmaxf(sv[w][0], sv[w][1]), fmaxf(sv[w][2], sv[w][3]));
-        mx = fmaxf(mx, MASK ? m4 : m4 * f[w][hh]);
-      }
-      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-      const float mn = fmaxf(m[hh], mx), ms = mn == -INFINITY ? 0.f : mn;
-      if (__any_sync(0xffffffffu, mn != m[hh])) {   // some row's maximum rose
-        const float a = ex2f(m[hh] - ms);
-        l[hh] *= a;
-        const float a0 = __shfl_sync(0xffffffffu, a, 8 * t), a1 = __shfl_sync(0xffffffffu, a, 8 * t + 4);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) { o[i][hh].x *= a0; o[i][hh].y *= a1; o[i][hh].z *= a0; o[i][hh].w *= a1; }
+        for (int e = 0; e < 2; ++e) {
+          v[w][e] = make_float2(s[w][hh][2 * e], s[w][hh][2 * e + 1]);
+          if (MASK) {
+            v[w][e] = mul2(v[w][e], f[w][hh]);
+            if (pos + x + 8 * e >= lim[hh].x) v[w][e].x = -INFINITY;
+            if (pos + x + 8 * e >= lim[hh].y) v[w][e].y = -INFINITY;
+          }
+        }
+        const float2 m2 = max2(v[w][0], v[w][1]);
+        mx = max2(mx, MASK ? m2 : mul2(m2, f[w][hh]));
+      }
+#pragma unroll
+      for (int k = 4; k < 32; k <<= 1) mx = max2(mx, make_float2(__shfl_xor_sync(0xffffffffu, mx.x, k), __shfl_xor_sync(0xffffffffu, mx.y, k)));
+      const float2 mn = max2(m[hh], mx), ms = make_float2(mn.x == -INFINITY ? 0.f : mn.x, mn.y == -INFINITY ? 0.f : mn.y);
+      if (__any_sync(0xffffffffu, mn.x != m[hh].x || mn.y != m[hh].y)) {   // some row's maximum rose
+        const float2 a = make_float2(ex2f(m[hh].x - ms.x), ex2f(m[hh].y - ms.y));
+        l[hh] = mul2(l[hh], a);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float2 lo = mul2(make_float2(o[i][hh].x, o[i][hh].y), a), hi = mul2(make_float2(o[i][hh].z, o[i][hh].w), a);
+          o[i][hh] = make_float4(lo.x, lo.y, hi.x, hi.y);
+        }
       }
       m[hh] = mn;
-      const float off = 15.f - ms;
+      const float2 off = make_float2(15.f - ms.x, 15.f - ms.y);
 #pragma unroll
       for (int w = 0; w < H; ++w) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          pw[w][hh][e] = ex2f(MASK ? sv[w][e] + off : fmaf(sv[w][e], f[w][hh], off));
-          l[hh] += pw[w][hh][e];
+        for (int e = 0; e < 2; ++e) {
+          const float2 y = MASK ? add2(v[w][e], off) : fma2(v[w][e], f[w][hh], off);
+          const float2 q = make_float2(ex2f(y.x), ex2f(y.y));
+          l[hh] = add2(l[hh], q);
+          pw[w][hh][2 * e] = q.x;
+          pw[w][hh][2 * e + 1] = q.y;
+          pb[w][hh][e] = movm_trans(pack_f16(q.x, q.y));
         }
-        pb[w][hh][0] = pack_f16(pw[w][hh][0], pw[w][hh][1]);
-        pb[w][hh][1] = pack_f16(pw[w][hh][2], pw[w][hh][3]);
       }
     }
   }
@@ -282,23 +322,24 @@ struct Running {
   __device__ __forceinline__ void leave(float *wo, float2 *wml, int x, int t, float times) {
 #pragma unroll
     for (int hh = 0; hh < NH; ++hh) {
-      float sum = l[hh], f_old = 0.f, f_new = 1.f, mn = m[hh];
-      sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-      sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-      if (JOIN) {
-        const float2 old = wml[x + 8 * hh];
-        mn = fmaxf(old.x, m[hh]);
-        f_old = mn == -INFINITY ? 1.f : ex2f(old.x - mn);
-        f_new = times * (mn == -INFINITY ? 1.f : ex2f(m[hh] - mn));
-        sum = old.y * f_old + sum * f_new;
-        __syncwarp();
-      }
-      if (t == 0) wml[x + 8 * hh] = make_float2(mn, sum);
+      float2 sum = l[hh];
+#pragma unroll
+      for (int k = 4; k < 32; k <<= 1) sum = add2(sum, make_float2(__shfl_xor_sync(0xffffffffu, sum.x, k), __shfl_xor_sync(0xffffffffu, sum.y, k)));
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        float *w = wo + (2 * t + c + 8 * hh) * kRowPad + 16 * x;
-        float fo = 0.f, fn = 1.f;
-        if (JOIN) { fo = __shfl_sync(0xffffffffu, f_old, 8 * t + 4 * c); fn = __shfl_sync(0xffffffffu, f_new, 8 * t + 4 * c); }
+        const int r = 2 * t + c + 8 * hh;
+        float mn = c ? m[hh].y : m[hh].x, total = c ? sum.y : sum.x, fo = 0.f, fn = 1.f;
+        if (JOIN) {
+          const float2 old = wml[r];
+          const float mine = mn;
+          mn = fmaxf(old.x, mine);
+          fo = mn == -INFINITY ? 1.f : ex2f(old.x - mn);
+          fn = times * (mn == -INFINITY ? 1.f : ex2f(mine - mn));
+          total = old.y * fo + total * fn;
+          __syncwarp();
+        }
+        if (x == 0) wml[r] = make_float2(mn, total);
+        float *w = wo + r * kRowPad + 16 * x;
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
           float4 y = c ? make_float4(o[i][hh].y, o[i][hh].w, o[i + 1][hh].y, o[i + 1][hh].w) : make_float4(o[i][hh].x, o[i][hh].z, o[i + 1][hh].x, o[i + 1][hh].z);
@@ -316,13 +357,16 @@ struct Running {
 // 16 places of the unfinished page (fp32), from pos on, joined to the warp's partial `times` over.  Elements go to fp16 times a power
 // of two of the tile's largest, values rounded (2^-11 of each), keys in two parts.  Out of line: its registers would be the tile loop's.
 template <int NH, int FMT>
-__device__ __noinline__ void tail_tile(const QAttParams &p, int row0, int h, int rows, int T, int lim0, int lim1, const float *kt, const float *vt, int pos, float times, float *wo, float2 *wml) {
+__device__ __noinline__ void tail_tile(const QAttParams &p, int row0, int h, int rows, int T, int2 lim0, int2 lim1, const float *kt, const float *vt, int pos, float times, float *wo, float2 *wml) {
   const int lane = threadIdx.x & 31, x = lane >> 2, t = lane & 3;
   uint32_t qf[NH][8][2], pb[1][NH][2];
-  float rs[NH], none[NH], pw[1][NH][4], s[2][4], f[1][NH];
-  int lim[NH];
+  float2 rs[NH], none[NH], f[1][NH];
+  float pw[1][NH][4], s[1][NH][4];
+  int2 lim[NH];
   lim[0] = lim0;
   lim[NH - 1] = NH == 1 ? lim0 : lim1;
+  uint4 raw[NH][4];
+  fetch_queries<NH>(p, row0, h, rows, x, t, raw);
   Running<NH> run;
   run.clear();
   float4 k[2][8];
@@ -349,7 +393,7 @@ __device__ __noinline__ void tail_tile(const QAttParams &p, int row0, int h, int
     for (int i = 0; i < 8; ++i)
       amax = fmaxf(amax, fmaxf(fmaxf(finite_abs(k[w][i].x), finite_abs(k[w][i].y)), fmaxf(finite_abs(k[w][i].z), finite_abs(k[w][i].w))));
   float up = power_to(warp_max(amax), 14);
-  load_queries<NH>(p, row0, h, rows, x, t, qf, rs, none);
+  take_queries<NH>(p, raw, t, qf, rs, none);
   bool odd = false;   // an infinity or a NaN
 #pragma unroll
   for (int w = 0; w < 2; ++w)
@@ -358,22 +402,28 @@ __device__ __noinline__ void tail_tile(const QAttParams &p, int row0, int h, int
       odd |= !(fabsf(k[w][i].x) < INFINITY && fabsf(k[w][i].y) < INFINITY && fabsf(k[w][i].z) < INFINITY && fabsf(k[w][i].w) < INFINITY);
   const bool finite_tile = !__any_sync(0xffffffffu, odd);
 #pragma unroll
-  for (int w = 0; w < 2; ++w) {
-    s[w][0] = s[w][1] = s[w][2] = s[w][3] = 0.f;
+  for (int hh = 0; hh < NH; ++hh) s[0][hh][0] = s[0][hh][1] = s[0][hh][2] = s[0][hh][3] = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {   // in two parts: 22 bits of each
-      const uint32_t a0 = qf[0][i][0], a1 = NH == 2 ? qf[NH - 1][i][0] : 0u, a2 = qf[0][i][1], a3 = NH == 2 ? qf[NH - 1][i][1] : 0u;
-      const float4 y = make_float4(k[w][i].x * up, k[w][i].y * up, k[w][i].z * up, k[w][i].w * up);
-      uint32_t lo = pack_f16(y.x, y.y), hi = pack_f16(y.z, y.w);
-      mma_f16(s[w], a0, a1, a2, a3, lo, hi);
-      const float2 l2 = __half22float2(*reinterpret_cast<__half2 *>(&lo)), h2 = __half22float2(*reinterpret_cast<__half2 *>(&hi));
-      const float4 rest = make_float4(y.x - l2.x, y.y - l2.y, y.z - h2.x, y.w - h2.y);
-      if (finite_tile) mma_f16(s[w], a0, a1, a2, a3, pack_f16(rest.x, rest.y), pack_f16(rest.z, rest.w));
+  for (int i = 0; i < 8; ++i) {   // in two parts: 22 bits of each
+    uint32_t a[4], rest[4];       // token x, x + 8; dims 0 1, 2 3 of the four
+#pragma unroll
+    for (int w = 0; w < 2; ++w)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float2 y = e ? make_float2(k[w][i].z * up, k[w][i].w * up) : make_float2(k[w][i].x * up, k[w][i].y * up);
+        a[w + 2 * e] = pack_f16(y.x, y.y);
+        const float2 z = __half22float2(*reinterpret_cast<__half2 *>(&a[w + 2 * e]));
+        rest[w + 2 * e] = pack_f16(y.x - z.x, y.y - z.y);
+      }
+#pragma unroll
+    for (int hh = 0; hh < NH; ++hh) {
+      mma_f16(s[0][hh], a[0], a[1], a[2], a[3], qf[hh][i][0], qf[hh][i][1]);
+      if (finite_tile) mma_f16(s[0][hh], rest[0], rest[1], rest[2], rest[3], qf[hh][i][0], qf[hh][i][1]);
     }
   }
 #pragma unroll
-  for (int hh = 0; hh < NH; ++hh) f[0][hh] = rs[hh] / up;
-  run.template weights<1, true>(s, f, lim, pos, t, pb, pw);
+  for (int hh = 0; hh < NH; ++hh) f[0][hh] = make_float2(rs[hh].x / up, rs[hh].y / up);
+  run.template weights<1, true>(s, f, lim, pos, x, pb, pw);
   amax = 0.f;
   odd = false;
 #pragma unroll
@@ -396,12 +446,12 @@ __device__ __noinline__ void tail_tile(const QAttParams &p, int row0, int h, int
   } else {   // token by token in fp32, so that a row takes nothing of a token that it does not see
 #pragma unroll 1
     for (int k2 = 0; k2 < 16 && pos + k2 < T; ++k2) {
-      const int e = (k2 & 1) + (k2 >> 3) * 2, from = (k2 & 7) >> 1;   // the weight's place: element e of the lanes with t = from
+      const int from = 4 * (k2 & 7) + t;   // who has the token's weights of rows 2 t, 2 t + 1
 #pragma unroll
       for (int hh = 0; hh < NH; ++hh) {
-        const float w = kUnit<FMT> * (e == 0 ? pw[0][hh][0] : (e == 1 ? pw[0][hh][1] : (e == 2 ? pw[0][hh][2] : pw[0][hh][3])));
-        const float w0 = __shfl_sync(0xffffffffu, w, 8 * t + from), w1 = __shfl_sync(0xffffffffu, w, 8 * t + 4 + from);
-        const bool s0 = pos + k2 < __shfl_sync(0xffffffffu, lim[hh], 8 * t), s1 = pos + k2 < __shfl_sync(0xffffffffu, lim[hh], 8 * t + 4);
+        const float w0 = kUnit<FMT> * __shfl_sync(0xffffffffu, k2 < 8 ? pw[0][hh][0] : pw[0][hh][2], from);
+        const float w1 = kUnit<FMT> * __shfl_sync(0xffffffffu, k2 < 8 ? pw[0][hh][1] : pw[0][hh][3], from);
+        const bool s0 = pos + k2 < lim[hh].x, s1 = pos + k2 < lim[hh].y;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const float2 y = *reinterpret_cast<const float2 *>(vt + k2 * LOCKS_D + 16 * x + 2 * i);
@@ -414,16 +464,17 @@ __device__ __noinline__ void tail_tile(const QAttParams &p, int row0, int h, int
   run.template leave<true>(wo, wml, x, t, times);
 }
 
-// Partials of CTAs c, c + step, .. c1 of the problem that begins in CTA c0: row r, four dims; loads four at a time
+// Partials of CTAs c, c + step, .. c1 of the problem that begins in CTA c0: row r, four dims; N loads at a time
+template <int N>
 __device__ __forceinline__ float4 join_partials(const QAttParams &p, int c0, int c, int c1, int step, int r, int d4, float &M, float &L) {
   M = -INFINITY;
   L = 0.f;
   float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (; c <= c1; c += 4 * step) {
-    float2 ml[4];
-    float4 y[4];
+  for (; c <= c1; c += N * step) {
+    float2 ml[N];
+    float4 y[N];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < N; ++i) {
       const int ci = c + i * step, s = 2 * ci + (ci == c0 ? 1 : 0);
       ml[i] = make_float2(-INFINITY, 0.f);
       y[i] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -433,7 +484,7 @@ __device__ __forceinline__ float4 join_partials(const QAttParams &p, int c0, int
       }
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < N; ++i) {
       const float mn = fmaxf(M, ml[i].x), fo = mn == -INFINITY ? 1.f : ex2f(M - mn), fn = mn == -INFINITY ? 1.f : ex2f(ml[i].x - mn);
       L = L * fo + ml[i].y * fn;
       a.x = a.x * fo + y[i].x * fn; a.y = a.y * fo + y[i].y * fn; a.z = a.z * fo + y[i].z * fn; a.w = a.w * fo + y[i].w * fn;
@@ -481,8 +532,8 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<NH>) kvq_token_kernel(con
   pdl_trigger();
   pdl_wait();
   Line line;
-  line.read(p, lane);
-  const int share = share_of(line.all, gridDim.x);
+  line.read(p, lane, gridDim.x);
+  const int share = line.share, lead = line.lead;
   if ((int64_t)share * blockIdx.x >= line.all) return;
   int u = share * blockIdx.x, b = -1, begin = 0;
   const int u_end = min((int64_t)u + share, (int64_t)line.all);
@@ -492,10 +543,10 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<NH>) kvq_token_kernel(con
   const uint32_t k_dst = cr * 128 + ((cc ^ (4 * (cr & 1))) << 4), v_dst = 2048 + cr * 128 + ((cc ^ (2 * (cr >> 1))) << 4);
   const int64_t st = CONTIG ? LOCKS_D : p.c.st, c_off = (int64_t)cr * st + cc * 16;
   while (u < u_end) {
-    if (b < 0 || u >= begin + places(p, req)) line.find(p, u, lane, b, begin, req);
-    const int span = kLead + req.pairs, prob = (u - begin) / span, prob_begin = begin + prob * span;   // problem of the request
-    const int seg0 = max(u - prob_begin - kLead, 0), seg1 = min(req.pairs, u_end - prob_begin - kLead);
-    u = prob_begin + kLead + max(seg1, 0);
+    if (b < 0 || u >= begin + line.places(p, req)) line.find(p, u, lane, b, begin, req);
+    const int span = lead + req.pairs, prob = (u - begin) / span, prob_begin = begin + prob * span;   // problem of the request
+    const int seg0 = max(u - prob_begin - lead, 0), seg1 = min(req.pairs, u_end - prob_begin - lead);
+    u = prob_begin + lead + max(seg1, 0);
     if (seg1 <= seg0) continue;   // (nothing but some of the problem's lead)
     const int h = prob % p.Hkv, rt = prob / p.Hkv, hkv = h / p.kvdiv, kv_heads = p.Hkv / p.kvdiv;
     const int j0 = rt * p.tile_tokens, toks = min(p.tile_tokens, req.n - j0), rows = toks * p.G;
@@ -546,6 +597,8 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<NH>) kvq_token_kernel(con
       r.easy = __ballot_sync(0xffffffffu, r.blk >= 0 && r.page * B + (tile & sub_mask) * 16 + 16 <= lim_min);
       return r;
     };
+    uint4 raw[NH][4];
+    fetch_queries<NH>(p, req.row0 + j0, h, rows, x, t, raw);
     Batch cur = resolve(0), next = cur;
     auto issue = [&](int j, const Batch &r) {   // a pair's copies
       uint8_t *dst = ring + (j % S) * kPair;
@@ -571,41 +624,47 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<NH>) kvq_token_kernel(con
 #pragma unroll
     for (int j = 0; j < S - 1; ++j) issue(j, cur);
     uint32_t qf[NH][8][2];
-    float rs[NH], start[NH];
-    load_queries<NH>(p, req.row0 + j0, h, rows, x, t, qf, rs, start);
-    int lim[NH];    // row x (+ 8) sees the first lim tokens
+    float2 rs[NH], start[NH];
+    take_queries<NH>(p, raw, t, qf, rs, start);
+    int2 lim[NH];    // rows 2 t, 2 t + 1 (+ 8) see the first lim tokens
 #pragma unroll
-    for (int hh = 0; hh < NH; ++hh) lim[hh] = x + 8 * hh < rows ? T - req.n + j0 + (x + 8 * hh) / p.G + 1 : T;
+    for (int hh = 0; hh < NH; ++hh) {
+      const int r = 2 * t + 8 * hh;
+      lim[hh] = make_int2(r < rows ? lim_min + r / p.G : T, r + 1 < rows ? lim_min + (r + 1) / p.G : T);
+    }
     Running<NH> run;
     run.clear();
 #pragma unroll
     for (int hh = 0; hh < NH; ++hh) {
-      if (FMT == LOCKS_KVQ_INT) rs[hh] *= 0x1p24f;
-      else start[hh] = 0.f;
+      if (FMT == LOCKS_KVQ_INT) rs[hh] = make_float2(rs[hh].x * 0x1p24f, rs[hh].y * 0x1p24f);
+      else start[hh] = make_float2(0.f, 0.f);
     }
-    // scores of a tile: two chains of four steps for each eight tokens
-    auto scores = [&](const uint8_t *kt, float (&s)[2][4]) {
+    // scores of a tile: two chains of four steps
+    auto scores = [&](const uint8_t *kt, float (&s)[NH][4]) {
+      float c[2][NH][4];
 #pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        float c[2][4];
+      for (int half = 0; half < 2; ++half) {
+        const uint32_t at = x * 128 + (((4 * half + t) ^ (4 * (x & 1))) << 4);
+        const uint4 y0 = *reinterpret_cast<const uint4 *>(kt + at), y1 = *reinterpret_cast<const uint4 *>(kt + at + 1024);
+        const uint32_t w0[4] = {y0.x, y0.y, y0.z, y0.w}, w1[4] = {y1.x, y1.y, y1.z, y1.w};
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const uint4 y = *reinterpret_cast<const uint4 *>(kt + (x + 8 * w) * 128 + (((4 * half + t) ^ (4 * (x & 1))) << 4));
-          const uint32_t word[4] = {y.x, y.y, y.z, y.w};
+        for (int i = 0; i < 4; ++i) {
+          const int k = 4 * half + i;
+          uint32_t a[4];   // token x, x + 8; dims 0 1, 2 3 of the four
+          halves<FMT>(kvq_flip<FMT>(w0[i]), a[0], a[2]);
+          halves<FMT>(kvq_flip<FMT>(w1[i]), a[1], a[3]);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int k = 4 * half + i;
-            uint32_t lo, hi;
-            halves<FMT>(kvq_flip<FMT>(word[i]), lo, hi);
-            const uint32_t a1 = NH == 2 ? qf[NH - 1][k][0] : 0u, a3 = NH == 2 ? qf[NH - 1][k][1] : 0u;
-            if (k == 0) mma_f16_from(c[0], qf[0][k][0], a1, qf[0][k][1], a3, lo, hi, start[0], start[0], start[NH - 1], start[NH - 1]);
-            else if (k == 4) mma_f16_from(c[1], qf[0][k][0], a1, qf[0][k][1], a3, lo, hi, 0.f, 0.f, 0.f, 0.f);
-            else mma_f16(c[half], qf[0][k][0], a1, qf[0][k][1], a3, lo, hi);
+          for (int hh = 0; hh < NH; ++hh) {
+            if (k == 0) mma_f16_from(c[0][hh], a[0], a[1], a[2], a[3], qf[hh][k][0], qf[hh][k][1], start[hh].x, start[hh].y, start[hh].x, start[hh].y);
+            else if (k == 4) mma_f16_from(c[1][hh], a[0], a[1], a[2], a[3], qf[hh][k][0], qf[hh][k][1], 0.f, 0.f, 0.f, 0.f);
+            else mma_f16(c[half][hh], a[0], a[1], a[2], a[3], qf[hh][k][0], qf[hh][k][1]);
           }
         }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[w][e] = c[0][e] + c[1][e];
       }
+#pragma unroll
+      for (int hh = 0; hh < NH; ++hh)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[hh][e] = c[0][hh][e] + c[1][hh][e];
     };
     auto values = [&](const uint8_t *vt, const uint32_t (&pb)[NH][2], const float2 (&fv)[NH]) {
       float2 from[NH];
@@ -649,18 +708,16 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<NH>) kvq_token_kernel(con
       const float ks[2] = {__shfl_sync(0xffffffffu, cur.ks, l), __shfl_sync(0xffffffffu, cur.ks, l + 1)};
       const float vs[2] = {__shfl_sync(0xffffffffu, cur.vs, l) * kScaleUnit<FMT>, __shfl_sync(0xffffffffu, cur.vs, l + 1) * kScaleUnit<FMT>};
       if (((cur.easy >> l) & 3) == 3) {
-        float s[4][4], f[2][NH], pw[2][NH][4];
+        float s[2][NH][4], pw[2][NH][4];
+        float2 f[2][NH];
         uint32_t pb[2][NH][2];
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
-          float sw[2][4];
-          scores(pair + w * kTile, sw);
+          scores(pair + w * kTile, s[w]);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) { s[2 * w][e] = sw[0][e]; s[2 * w + 1][e] = sw[1][e]; }
-#pragma unroll
-          for (int hh = 0; hh < NH; ++hh) f[w][hh] = rs[hh] * ks[w];
+          for (int hh = 0; hh < NH; ++hh) f[w][hh] = make_float2(rs[hh].x * ks[w], rs[hh].y * ks[w]);
         }
-        run.template weights<2, false>(s, f, lim, 0, t, pb, pw);
+        run.template weights<2, false>(s, f, lim, 0, x, pb, pw);
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
           float2 fv[NH];
@@ -677,17 +734,16 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<NH>) kvq_token_kernel(con
             if (__shfl_sync(0xffffffffu, cur.blk, l + w) == kUnfinished) tails += 1ull << (16 * sub);
             continue;
           }
-          float s[2][4], f[1][NH], pw[1][NH][4];
+          float s[1][NH][4], pw[1][NH][4];
+          float2 f[1][NH], fv[NH];
           uint32_t pb[1][NH][2];
-          float2 fv[NH];
-          scores(pair + w * kTile, s);
+          scores(pair + w * kTile, s[0]);
 #pragma unroll
           for (int hh = 0; hh < NH; ++hh) {   // rows that see nothing of the tile take nothing of it, not even a NaN that its scale may be
-            f[0][hh] = rs[hh] * (w ? ks[1] : ks[0]);
-            fv[hh].x = pos < __shfl_sync(0xffffffffu, lim[hh], 8 * t) ? (w ? vs[1] : vs[0]) : 0.f;
-            fv[hh].y = pos < __shfl_sync(0xffffffffu, lim[hh], 8 * t + 4) ? (w ? vs[1] : vs[0]) : 0.f;
+            f[0][hh] = make_float2(rs[hh].x * (w ? ks[1] : ks[0]), rs[hh].y * (w ? ks[1] : ks[0]));
+            fv[hh] = make_float2(pos < lim[hh].x ? (w ? vs[1] : vs[0]) : 0.f, pos < lim[hh].y ? (w ? vs[1] : vs[0]) : 0.f);
           }
-          run.template weights<1, true>(s, f, lim, pos, t, pb, pw);
+          run.template weights<1, true>(s, f, lim, pos, x, pb, pw);
           values(pair + w * kTile + 2048, pb[0], fv);
         }
       }
@@ -732,7 +788,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<NH>) kvq_token_kernel(con
       }
     }
     if (!whole && p.done) {   // the last of the problem's CTAs puts its partials together, in their order
-      const int c0 = (prob_begin + kLead) / share, c1 = (prob_begin + kLead + req.pairs - 1) / share;
+      const int c0 = (prob_begin + lead) / share, c1 = (prob_begin + lead + req.pairs - 1) / share;
       __syncthreads();
       if (tid == 0) {
         __threadfence();   // what the CTA has written, which the barrier orders before
@@ -744,7 +800,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<NH>) kvq_token_kernel(con
         for (int i = tid; i < rows * (LOCKS_D / 4); i += kThreads) {
           const int r = i >> 5, d4 = 4 * (i & 31);
           float M, L;
-          const float4 a = join_partials(p, c0, c0, c1, 1, r, d4, M, L);
+          const float4 a = join_partials<8>(p, c0, c0, c1, 1, r, d4, M, L);
           finish_dims<FMT>(p, row_of(r), d4, a, M, L);
         }
         if (tid == 0) p.done[c0] = 0;   // ready for the next launch
@@ -754,11 +810,11 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<NH>) kvq_token_kernel(con
   }
 }
 
-// Problems that many CTAs share: a CTA per output row puts their partials together, a warp every fourth of them.
+// Problems that many CTAs share: a CTA per output row puts their partials together, a warp every eighth of them.
 template <int FMT>
-__global__ void __launch_bounds__(kThreads) kvq_join_kernel(const __grid_constant__ QAttParams p, int ctas) {
-  __shared__ float4 a_s[kWarps][32];
-  __shared__ float2 ml_s[kWarps];
+__global__ void __launch_bounds__(32 * kJoinWarps) kvq_join_kernel(const __grid_constant__ QAttParams p, int ctas) {
+  __shared__ float4 a_s[kJoinWarps][32];
+  __shared__ float2 ml_s[kJoinWarps];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int hq = blockIdx.x, row = blockIdx.y, h = hq / p.G;
   pdl_trigger();
@@ -774,29 +830,29 @@ __global__ void __launch_bounds__(kThreads) kvq_join_kernel(const __grid_constan
   const int j = row - req.row0;
   if (j >= req.n) return;   // (offsets out of range)
   Line line;
-  line.read(p, lane);
-  const int share = share_of(line.all, ctas);
+  line.read(p, lane, ctas);
+  const int share = line.share;
   int before = 0;   // places of the requests before
   if (b < 32) {
-    before = __shfl_sync(0xffffffffu, line.end - places(p, line.r), b);
+    before = __shfl_sync(0xffffffffu, line.end - line.places(p, line.r), b);
   } else {
     before = __shfl_sync(0xffffffffu, line.end, 31);
-    for (int b0 = 32; b0 < b; b0 += 32) before += __reduce_add_sync(0xffffffffu, b0 + lane < b ? places(p, request_at(p, b0 + lane)) : 0);
+    for (int b0 = 32; b0 < b; b0 += 32) before += __reduce_add_sync(0xffffffffu, b0 + lane < b ? line.places(p, request_at(p, b0 + lane)) : 0);
   }
   const int rt = j / p.tile_tokens, r = (j - rt * p.tile_tokens) * p.G + hq - h * p.G;
-  const int at = before + (rt * p.Hkv + h) * (kLead + req.pairs) + kLead;   // its first pair
+  const int at = before + (rt * p.Hkv + h) * (line.lead + req.pairs) + line.lead;   // its first pair
   const int c0 = at / share, c1 = (at + req.pairs - 1) / share;
   if (c0 == c1) return;     // finished by its CTA
   float M, L;
-  const float4 a = join_partials(p, c0, c0 + warp, c1, kWarps, r, 4 * lane, M, L);
+  const float4 a = join_partials<8>(p, c0, c0 + warp, c1, kJoinWarps, r, 4 * lane, M, L);
   a_s[warp][lane] = a;
   if (lane == 0) ml_s[warp] = make_float2(M, L);
   __syncthreads();
   if (warp) return;
   M = -INFINITY; L = 0.f;
-  for (int w = 0; w < kWarps; ++w) M = fmaxf(M, ml_s[w].x);
+  for (int w = 0; w < kJoinWarps; ++w) M = fmaxf(M, ml_s[w].x);
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int w = 0; w < kWarps; ++w) {
+  for (int w = 0; w < kJoinWarps; ++w) {
     const float f = M == -INFINITY ? 1.f : ex2f(ml_s[w].x - M);
     const float4 y = a_s[w][lane];
     L += ml_s[w].y * f;
@@ -850,7 +906,7 @@ extern "C" int locks_kvq_attend(locks_ctx *ctx, const void *q, const int32_t *cu
 #undef KVQ_TOKEN
   if ((rc = locks_check_launch(ctx)) != LOCKS_OK || !join) return rc;
   const dim3 rows(p.Hq, num_tokens);
-  if (kv->fmt == LOCKS_KVQ_INT) locks_launch_pdl(kvq_join_kernel<LOCKS_KVQ_INT>, rows, dim3(kThreads), 0, (cudaStream_t)stream, p, ctas);
-  else locks_launch_pdl(kvq_join_kernel<LOCKS_KVQ_FLOAT>, rows, dim3(kThreads), 0, (cudaStream_t)stream, p, ctas);
+  if (kv->fmt == LOCKS_KVQ_INT) locks_launch_pdl(kvq_join_kernel<LOCKS_KVQ_INT>, rows, dim3(32 * kJoinWarps), 0, (cudaStream_t)stream, p, ctas);
+  else locks_launch_pdl(kvq_join_kernel<LOCKS_KVQ_FLOAT>, rows, dim3(32 * kJoinWarps), 0, (cudaStream_t)stream, p, ctas);
   return locks_check_launch(ctx);
 }
