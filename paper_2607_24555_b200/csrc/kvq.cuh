@@ -35,6 +35,9 @@ static inline int kvq_check(const locks_ctx *c, const locks_kvq *kv, int batch) 
   return LOCKS_OK;
 }
 
+// attention of many rows per KV head (kvq_chunk.cu); cu is not null
+int locks_launch_kvq_chunk(locks_ctx *c, const void *q, const int32_t *cu, int n, const locks_kvq *kv, int batch, void *out, float *lse, cudaStream_t st);
+
 // token attention: partials of the problems that several CTAs share, of whom each leaves at most two
 static inline size_t kvq_part_floats() { return (size_t)2 * KVQ_SLOT_BOUND * KVQ_ROWS * LOCKS_D; }
 static inline size_t kvq_ml_floats() { return (size_t)2 * KVQ_SLOT_BOUND * KVQ_ROWS * 2; }

@@ -877,6 +877,14 @@ extern "C" int locks_kvq_attend(locks_ctx *ctx, const void *q, const int32_t *cu
   if (ctx->cfg.combine == LOCKS_COMBINE_PER_HEAD && page_ids) { p.kvdiv = p.G; p.Hkv = p.Hq; p.G = 1; }   // a page table per query head
   p.sub_shift = ctx->B == 64 ? 2 : (ctx->B == 32 ? 1 : 0);
   p.c2 = ctx->cfg.sm_scale * kLog2e;
+  // Chunks of prompts: 128 rows a tile, where that gives every SM a tile, or where the line of the other form may not fit 32 bits
+  const int64_t problem = (((int64_t)(page_ids ? p.kbud : p.c.Pmax) << p.sub_shift) + 1) / 2 + kMostLead;   // places at most
+  const bool fits = (batch + (cu_tokens ? (int64_t)num_tokens : 0)) * p.Hkv * problem <= INT32_MAX;
+  if (cu_tokens && (!fits || (int64_t)num_tokens * p.G / 128 * p.Hkv >= ctx->num_sms)) {
+    ctx->last_launches = 0;
+    return locks_launch_kvq_chunk(ctx, q, cu_tokens, num_tokens, kv, batch, out, lse, (cudaStream_t)stream);
+  }
+  if (!fits) return LOCKS_ERR_TOO_LARGE;
   // 8 rows a tile where a request's rows fit on average, else 16
   const bool wide = p.G > 8 || (int64_t)num_tokens * p.G > (int64_t)8 * batch;
   p.tile_tokens = (wide ? 16 : 8) / p.G;

@@ -224,7 +224,7 @@ static inline int locks_check_launch(locks_ctx *c) {
 // sets them on each.  Thread-safe.
 enum { LOCKS_ATTR_SELECT = 0, LOCKS_ATTR_ATTEND = 1, LOCKS_ATTR_EXACT = 3, LOCKS_ATTR_SCAN = 8,
        LOCKS_ATTR_BUILD_PAGE = 20 /* + page size / 32 */, LOCKS_ATTR_BUILD_WIDE = 24 /* + format */, LOCKS_ATTR_SCAN_WIDE = 28 /* + rank / 4 */, LOCKS_ATTR_BUILD_CODES = 32 /* + format */,
-       LOCKS_ATTR_KVQ = 40 /* + 4 (rows / 8 - 1) + 2 format + contiguous */ };
+       LOCKS_ATTR_KVQ = 40 /* + 4 (rows / 8 - 1) + 2 format + contiguous */, LOCKS_ATTR_KVQ_CHUNK = 48 /* + format */ };
 bool locks_attrs_needed(int family);
 
 // ---------------------------------------------------------------- I4 blob geometry (d = 128; B = 16 unless given)

@@ -104,7 +104,11 @@ def sequence(kvq, b, h, T, B, pages=None):
 def attend(q, kvq, lens, new, Hkv, B, ids=None, cnt=None, per_head=False):
     """(out, lse, bound): 64-bit attention, and what the kernel may be off by: its result's rounding to bf16 (2^-8 of it); weights in
     fp16 (2^-11 of each, 2^-25 at least: below fp16's normal numbers); the unfinished page's elements in fp16 (2^-11 of each, in the
-    scores and in the values); scores summed in fp32 (128 products, each sum within 2^-23: 2^-16 of the sum of magnitudes)."""
+    scores and in the values); scores summed in fp32 (128 products, each sum within 2^-23: 2^-16 of the sum of magnitudes).
+    The few-token form multiplies weights by code + 128 (up to 255, times the page's scale) and takes 128 sum of weights off in the same
+    accumulator: 16 products and a start, each cut off at 2^-23 of the largest, which is at most 255 times its weight: so a
+    tile's sum is off by at most 17 x 255 x 2^-23 of weight times scale, which no small output makes smaller.  (Seen: a token of
+    weight 0.9988 whose code is 0, others' values adding up to 8.2e-5 and off by 1.6e-6, with 17 x 255 x 2^-23 x 0.024 = 1.2e-5.)"""
     n, Hq = q.shape[0], q.shape[1]
     G = Hq // Hkv
     out, lse = torch.zeros(n, Hq, D, dtype=torch.float64), torch.full((n, Hq), -math.inf, dtype=torch.float64)
@@ -113,27 +117,31 @@ def attend(q, kvq, lens, new, Hkv, B, ids=None, cnt=None, per_head=False):
     row = 0
     for b, (T, m) in enumerate(zip(lens, new)):
         for hh in range(Hq if per_head else Hkv):
-            h, heads = (hh // G, [hh]) if per_head else (hh, range(hh * G, hh * G + G))
+            h, heads = (hh // G, slice(hh, hh + 1)) if per_head else (hh, slice(hh * G, hh * G + G))
             pages = None if ids is None else [int(p) for p in ids[b, hh, :int(cnt[b, hh])]]
             k, v, pos = sequence(kvq, b, h, T, B, pages)
-            in_tail = pos >= T // B * B
-            for j in range(m):
-                see = pos < T - m + j + 1
-                if not bool(see.any()):
-                    continue
-                kk, vv, tail = k[see], v[see], in_tail[see]
-                for g in heads:
-                    qq = q64[row + j, g]
-                    s = kk @ qq * sm
-                    lse[row + j, g] = torch.logsumexp(s, 0)
-                    p = torch.softmax(s, 0)
-                    o = p @ vv
-                    out[row + j, g] = o
-                    mag = (kk.abs() @ qq.abs()) * sm
-                    d = mag * (2.0 ** -16 + tail * 2.0 ** -11) + 2.0 ** -20   # of a score; and of the exponential
-                    w = (p * torch.expm1(d)) @ (vv.abs() + o.abs())
-                    low = 2.0 ** -25 * torch.exp(s.max() - lse[row + j, g]) * vv.abs().sum(0)
-                    bound[row + j, g] = 2.0 ** -8 * o.abs() + 1.01 * (w + 2.0 ** -11 * (p @ vv.abs()) + 2.0 ** -11 * ((p * tail) @ vv.abs()) + low) + 1e-30
-                    lse_bound[row + j, g] = (p * d).sum() + 2.0 ** -20 * (1 + abs(float(lse[row + j, g])))
+            vs = torch.tensor([0.0 if int(i) >= T // B * B else float(kvq.v_scale[int(kvq.block_table[b, int(i) // B]), h]) for i in pos[::16]],
+                              dtype=torch.float64).repeat_interleave(16)[:len(pos)]
+            if m == 0 or len(pos) == 0:
+                continue
+            qq = q64[row:row + m, heads]                                  # [m, g, D]
+            see = (pos[None] < (T - m + 1 + torch.arange(m))[:, None])    # [m, tokens]
+            some = see.any(1)
+            s = (qq @ k.T * sm).masked_fill(~see[:, None], -math.inf)
+            ll = torch.logsumexp(s, 2)
+            p = torch.exp(s - ll.masked_fill(~some[:, None], 0.0)[..., None])
+            o = p @ v
+            mag = (qq.abs() @ k.abs().T) * sm
+            tail = (pos >= T // B * B).to(torch.float64)
+            d = mag * (2.0 ** -16 + tail * 2.0 ** -11) + 2.0 ** -20       # of a score; and of the exponential
+            pd = p * torch.expm1(d)
+            w = pd @ v.abs() + pd.sum(2, keepdim=True) * o.abs()
+            top = s.max(2).values
+            low = 2.0 ** -25 * torch.exp(torch.where(some[:, None], top - ll, 0.0))[..., None] * (see.to(torch.float64) @ v.abs())[:, None]
+            err = 2.0 ** -8 * o.abs() + 1.01 * (w + 2.0 ** -11 * (p @ v.abs()) + 2.0 ** -11 * ((p * tail) @ v.abs()) + low) + 17 * 255 * 2.0 ** -23 * (p @ vs)[..., None] + 1e-30
+            lerr = (p * d).sum(2) + 2.0 ** -20 * (1 + ll.abs())
+            sel = some.nonzero()[:, 0]
+            out[row + sel, heads], lse[row + sel, heads] = o[sel], ll[sel]
+            bound[row + sel, heads], lse_bound[row + sel, heads] = err[sel], lerr[sel]
         row += m
     return out, lse, bound, lse_bound

@@ -354,6 +354,37 @@ def test_attend_several_tokens(Hq, Hkv, lens, new, pad, B):
     assert ctx.locks_poll_status() == 0
 
 
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("B,layout", [(16, "HND"), (32, "NHD"), (64, "HND")])
+@pytest.mark.parametrize("Hq,Hkv,lens,new,pad", [
+    (64, 16, [130, 45, 300], [100, 45, 200], 3), (128, 16, [90, 64, 33], [90, 60, 1], 0), (176, 16, [200, 20], [140, 0], 1), (256, 16, [16, 81, 70], [16, 1, 64], 0),
+    (20, 20, [1000], [1000], 2)])
+def test_attend_chunks(Hq, Hkv, lens, new, pad, B, layout, fmt):
+    """Enough rows per KV head for the form with 128 rows a tile."""
+    ctx, kvq, q, out, lse = run_attend(Hq, Hkv, B, fmt, layout, lens, new, pad)
+    check_attend(Hq, Hkv, B, lens, new, kvq, q, out, lse)
+    assert ctx.locks_poll_status() == 0
+
+
+def test_attend_long_sequences():
+    """Shares of hundreds of tiles, in both forms of the token kernel, against torch in 64 bits on the GPU."""
+    for Hq, Hkv, lens in ((32, 8, [300_000]), (32, 2, [700_000, 40_001]), (8, 8, [120_001, 7, 90_000, 33])):
+        ctx, kvq, q, out, lse = run_attend(Hq, Hkv, 16, "int8", "HND", lens, [1] * len(lens))
+        for b, t in enumerate(lens):
+            for h in range(0, Hkv, max(1, Hkv // 2)):
+                blocks = kvq.block_table[b, :t // 16].long()
+                k, v = [torch.cat([(getattr(kvq, n)[blocks, h].double() * getattr(kvq, n + "_scale")[blocks, h].double()[:, None, None]).flatten(0, 1),
+                                   getattr(kvq, n + "_tail")[b, h, :t % 16].double()]) for n in ("k", "v")]
+                g = slice(h * Hq // Hkv, (h + 1) * Hq // Hkv)
+                s = q[b, g].double() @ k.T * 128 ** -0.5
+                want, ll = torch.softmax(s, 1) @ v, torch.logsumexp(s, 1)
+                # 2^-8 of the result, 2^-11 of each weight; scores within 2^-16 of their magnitudes, which are below 200
+                tol = 2.0 ** -8 * want.abs() + (2.0 ** -11 + 200 * 2.0 ** -16) * 1.1 * (torch.softmax(s, 1) @ v.abs()) + 1e-4
+                assert float(((out[b, g].double() - want).abs() - tol).max()) <= 0
+                assert float((lse[b, g].double() - ll).abs().max()) <= 200 * 2.0 ** -16
+        assert ctx.locks_poll_status() == 0
+
+
 @pytest.mark.parametrize("B,combine", [(16, 0), (32, 0), (64, 0), (16, locks.COMBINE_PER_HEAD)])
 def test_attend_listed_pages(B, combine):
     Hq, Hkv, lens, k = 8, 2, [16 * 40 + 3, 64, 30, 500, 0], 6
@@ -393,36 +424,41 @@ def test_attend_queries_of_any_size(scale):
     check_attend(8, 2, 16, lens, [1, 1], kvq, q, out, lse)
 
 
-def test_attend_infinities_and_nan():
+@pytest.mark.parametrize("Hq,Hkv,n0", [(8, 2, 20), (64, 16, 300)])
+def test_attend_infinities_and_nan(Hq, Hkv, n0):
     """Stale rows behind the last token are not looked at; a poisoned page makes NaN of what attends it and of nothing else; an
     infinite value in the unfinished page stays infinite, for the tokens that see it."""
+    G = Hq // Hkv
+    lens, new = ([37, 49], [3, 1]) if n0 == 20 else ([325, 49], [310, 30])
+
     def stale(kvq):
         for n in ("k_tail", "v_tail"):
             getattr(kvq, n)[0, :, 5:] = float("nan")
             getattr(kvq, n)[1, :, 1:] = float("inf")
-        used = set(kvq.block_table[0, :2].tolist() + kvq.block_table[1, :3].tolist())
+        used = set(kvq.block_table[0, :lens[0] // 16].tolist() + kvq.block_table[1, :lens[1] // 16].tolist())
         for i in range(kvq.k.shape[0]):
             if i not in used:
                 kvq.k_scale[i] = kvq.v_scale[i] = float("nan")
-    lens = [37, 49]
-    ctx, kvq, q, out, lse = run_attend(8, 2, 16, "int8", "HND", lens, [3, 1], change=stale)
-    check_attend(8, 2, 16, lens, [3, 1], kvq, q, out, lse)
+    ctx, kvq, q, out, lse = run_attend(Hq, Hkv, 16, "int8", "HND", lens, new, change=stale)
+    check_attend(Hq, Hkv, 16, lens, new, kvq, q, out, lse)
 
     for which in ("k_scale", "v_scale"):
         def poison(kvq):
             getattr(kvq, which)[int(kvq.block_table[0, 1]), 0] = float("nan")   # places 16 .. 31, head 0
-        ctx, kvq, q, out, lse = run_attend(8, 2, 16, "int8", "HND", [34, 40], [20, 1], change=poison)
-        assert bool(torch.isnan(out[2:20, :4]).all()), which
+        T = n0 + 14   # the new tokens' places are 14 ..
+        ctx, kvq, q, out, lse = run_attend(Hq, Hkv, 16, "int8", "HND", [T, 40], [n0, 1], change=poison)
+        assert bool(torch.isnan(out[2:n0, :G]).all()), which
         fine = out.clone()
-        fine[2:20, :4] = 0
+        fine[2:n0, :G] = 0
         assert not bool(torch.isnan(fine).any()), which
 
     def infinite(kvq):
-        kvq.v_tail[0, 1, 2, 9] = float("inf")     # place 34 of request 0
-    ctx, kvq, q, out, lse = run_attend(8, 2, 16, "e4m3", "HND", [37, 40], [4, 1], change=infinite, q_scale=0.1)
+        kvq.v_tail[0, 1, 2, 9] = float("inf")     # the third place of the unfinished page of request 0
+    T, n = (37, 4) if n0 == 20 else (325, 310)
+    ctx, kvq, q, out, lse = run_attend(Hq, Hkv, 16, "e4m3", "HND", [T, 40], [n, 1], change=infinite, q_scale=0.1)
     hit = torch.isinf(out)
     want = torch.zeros_like(hit)
-    want[1:4, 4:, 9] = True                        # the new tokens at places 34, 35, 36
+    want[n - (T - T // 16 * 16 - 2):n, G:2 * G, 9] = True
     assert torch.equal(hit, want) and not bool(torch.isnan(out).any())
 
 
