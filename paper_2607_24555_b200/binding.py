@@ -1,7 +1,9 @@
-"""ctypes binding of liblocks.so.  Names mirror include/locks.h; tensors are torch CUDA tensors."""
+"""Binding of liblocks.so (ctypes; calls that a serving loop makes per layer and step: natively, csrc/calls.cpp).  Names mirror
+include/locks.h; tensors are torch CUDA tensors."""
 from __future__ import annotations
 
 import ctypes as C
+import importlib.util
 import os
 from dataclasses import dataclass
 
@@ -67,6 +69,7 @@ class Rotary(C.Structure):
 
 
 _lib = None
+_calls_module = None
 
 
 def library_path() -> str:
@@ -142,6 +145,23 @@ def lib():
             getattr(L, fn).restype = C.c_int
         _lib = L
     return _lib
+
+
+def calls():
+    """The native marshalling module (_calls.so, built in-tree with the library), bound to the library's functions."""
+    global _calls_module
+    if _calls_module is None:
+        path = os.path.join(_HERE, "_calls.so")
+        if not os.path.exists(path):
+            raise LocksError(f"{path} is missing: run `python -m paper_2607_24555_b200.build`")
+        spec = importlib.util.spec_from_file_location(__package__ + "._calls", path)
+        m = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(m)
+        L = lib()
+        m.bind(LocksError, *[C.cast(getattr(L, f), C.c_void_p).value for f in
+                             ("locks_rope", "locks_append_rows", "locks_kvq_append", "locks_kvq_attend", "locks_kvq_build_summaries", "locks_strerror")])
+        _calls_module = m
+    return _calls_module
 
 
 def locks_strerror(code: int) -> str:
@@ -281,23 +301,6 @@ class KVView:
                   self.seq_lens.data_ptr())
 
 
-class _Device:
-    """Makes a device current for a call, if it is not (a context's workspace and attributes belong to its device)."""
-    __slots__ = ("index", "was")
-
-    def __init__(self, device):
-        self.index = device.index
-
-    def __enter__(self):
-        self.was = torch.cuda.current_device()
-        if self.was != self.index:
-            torch.cuda.set_device(self.index)
-
-    def __exit__(self, *exc):
-        if self.was != self.index:
-            torch.cuda.set_device(self.was)
-
-
 class Context:
     """Owns a locks_ctx and its torch-allocated workspace.  Methods mirror the C entry points."""
 
@@ -306,7 +309,6 @@ class Context:
         self.device = torch.device(device)
         if self.device.type == "cuda" and self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
-        self._dtype = torch.bfloat16 if cfg.q_dtype == BF16 else torch.float32
         L = lib()
         nbytes = locks_workspace_bytes(cfg)
         if nbytes == 0:
@@ -319,9 +321,14 @@ class Context:
             h = C.c_void_p()
             _check(L.locks_create(C.byref(cfg), base, nbytes, C.byref(h)), "locks_create")
         self.handle = h
+        self._calls = calls()
+        self._call = self._calls.context(h.value, cfg.num_q_heads, cfg.num_kv_heads, cfg.max_batch, cfg.max_pages_per_seq, cfg.page_size, self.k,
+                                         self.device.index, cfg.combine == COMBINE_PER_HEAD, self.summary_bytes, cfg.q_dtype == BF16)
 
     def close(self):
         if self.handle:
+            if getattr(self, "_call", None) is not None:
+                self._calls.close(self._call)
             lib().locks_destroy(self.handle)
             self.handle = None
 
@@ -425,111 +432,31 @@ class Context:
                                             _ptr(summaries), batch, _ptr(out_host), _ptr(page_ids_host),
                                             _ptr(page_count_host), _stream(stream)), "locks_decode_step_host")
 
-    # ---- rotary positions, appends and the 8-bit cache.  Tensors are checked here: type, shape, strides, device.
-    def _rows(self, t, heads, n, what):
-        _need(t.dim() == 3 and t.shape[0] == n and t.shape[1] == heads and t.shape[2] == 128 and t.stride(2) == 1,
-              f"{what}: [tokens, {heads}, 128] with contiguous dims expected, got {tuple(t.shape)}")
-        _need(t.dtype == self._dtype and t.device == self.device, f"{what}: {self._dtype} on {self.device} expected")
-        return C.byref(Rows(t.data_ptr(), t.stride(0), t.stride(1)))
-
-    def _ints(self, t, shape, what):
-        if t is None:
-            return None
-        _need(t.dtype == torch.int32 and tuple(t.shape) == shape and t.is_contiguous() and t.device == self.device,
-              f"{what}: contiguous int32 {shape} on {self.device} expected")
-        return t.data_ptr()
-
-    def _launch(self, stream):
-        """The stream to launch on, of this context's device."""
-        if stream is None:
-            return torch.cuda.current_stream(self.device).cuda_stream
-        return stream if isinstance(stream, int) else stream.cuda_stream
-
-    def _positions(self, rotary, positions, n):
-        if positions is None:
-            return None
-        if positions.dim() == 1:
-            positions = positions[None]
-        return self._ints(positions, (rotary.num_axes, n), "positions")
-
-    def _view_ok(self, view, batch, what):
-        c = self.cfg
-        _need(view.k.device == self.device, f"{what}: a cache on {self.device} expected")
-        _need(1 <= batch <= c.max_batch and view.seq_lens.shape[0] >= batch and view.block_table.shape[0] >= batch and
-              view.block_table.shape[1] == c.max_pages_per_seq, f"{what}: batch, lengths or block table do not fit the configuration")
-
-    def _kvq_ok(self, kvq, batch, what):
-        self._view_ok(kvq, batch, what)
-        _need(tuple(kvq.k.shape[1:]) == (self.cfg.num_kv_heads, self.cfg.page_size, 128) and kvq.k_tail.shape[0] >= batch,
-              f"{what}: the cache's heads, page size or tails do not fit the configuration")
-
+    # ---- rotary positions, appends and the 8-bit cache: checked (type, shape, strides, device) and marshalled natively, in csrc/calls.cpp
     def locks_rope(self, rotary, positions, q, q_out, k=None, k_out=None, stream=None):
         """Rotate q [tokens, Hq, 128] into q_out and k [tokens, Hkv, 128] into k_out (either pair may be None; in place: pass a
         tensor twice).  positions: int32 [axes, tokens], or [tokens] with one axis."""
-        c, L = self.cfg, lib()
-        _need(rotary is not None and positions is not None, "locks_rope: rotary and positions are needed")
-        _need((q is None) == (q_out is None) and (k is None) == (k_out is None) and (q is not None or k is not None), "locks_rope: q with q_out, k with k_out")
-        n = (q if q is not None else k).shape[0]
-        r = [None if t is None else self._rows(t, h, n, "locks_rope") for t, h in
-             ((q, c.num_q_heads), (q_out, c.num_q_heads), (k, c.num_kv_heads), (k_out, c.num_kv_heads))]
-        with _Device(self.device):
-            _check(L.locks_rope(self.handle, C.byref(rotary), self._positions(rotary, positions, n), n, *r, self._launch(stream)), "locks_rope")
-
-    def _append(self, fn, what, kv, k_new, v_new, batch, rotary, positions, q, q_out, cu_tokens, stream):
-        c, n = self.cfg, k_new.shape[0]
-        _need(rotary is not None or (q is None and q_out is None and positions is None), f"{what}: q and positions go with a rotary description")
-        _need((q is None) == (q_out is None), f"{what}: q with q_out")
-        r = [None if t is None else self._rows(t, h, n, what) for t, h in
-             ((q, c.num_q_heads), (q_out, c.num_q_heads), (k_new, c.num_kv_heads), (v_new, c.num_kv_heads))]
-        cu = self._ints(cu_tokens, (batch + 1,), f"{what}: cu_tokens")
-        pos = None if positions is None else self._positions(rotary, positions, n)
-        s = kv.struct()
-        with _Device(self.device):
-            _check(fn(self.handle, None if rotary is None else C.byref(rotary), pos, cu, n, *r, C.byref(s), batch, self._launch(stream)), what)
+        self._calls.rope(self._call, rotary, positions, q, q_out, k, k_out, stream)
 
     def locks_append_rows(self, k_new, v_new, kv: KVView, batch, rotary=None, positions=None, q=None, q_out=None, cu_tokens=None,
                           stream=None):
         """Append k_new, v_new [tokens, Hkv, 128] (keys rotated, if there is a rotary description) to the cache and rotate q into
         q_out.  kv.seq_lens counts the new tokens already; cu_tokens: see include/locks.h."""
-        self._view_ok(kv, batch, "locks_append_rows")
-        _need(kv.k.dtype == kv.v.dtype == self._dtype and kv.v.device == self.device, f"locks_append_rows: a {self._dtype} cache on {self.device} expected")
-        self._append(lib().locks_append_rows, "locks_append_rows", kv, k_new, v_new, batch, rotary, positions, q, q_out, cu_tokens, stream)
+        self._calls.append_rows(self._call, k_new, v_new, kv, batch, rotary, positions, q, q_out, cu_tokens, stream)
 
     def locks_kvq_append(self, k_new, v_new, kvq: KVQView, batch, rotary=None, positions=None, q=None, q_out=None, cu_tokens=None,
                          stream=None):
         """locks_append_rows for the 8-bit cache: complete pages as codes, the unfinished one in the tails."""
-        self._kvq_ok(kvq, batch, "locks_kvq_append")
-        self._append(lib().locks_kvq_append, "locks_kvq_append", kvq, k_new, v_new, batch, rotary, positions, q, q_out, cu_tokens, stream)
+        self._calls.kvq_append(self._call, k_new, v_new, kvq, batch, rotary, positions, q, q_out, cu_tokens, stream)
 
     def locks_kvq_attend(self, q, kvq: KVQView, batch, out, lse=None, page_ids=None, page_count=None, cu_tokens=None, stream=None):
         """Attention of q [tokens, Hq, 128] over the 8-bit cache into out; one token per request (all pages, or page_ids and
         page_count of locks_select), or with cu_tokens several, each seeing what is before it."""
-        c, n = self.cfg, q.shape[0]
-        self._kvq_ok(kvq, batch, "locks_kvq_attend")
-        for t in (q, out):
-            _need(t.shape == (n, c.num_q_heads, 128) and t.is_contiguous() and t.dtype == self._dtype and t.device == self.device,
-                  f"locks_kvq_attend: q and out are contiguous {self._dtype} [tokens, {c.num_q_heads}, 128] on {self.device}")
-        _need(lse is None or (lse.shape == (n, c.num_q_heads) and lse.is_contiguous() and lse.dtype == torch.float32 and lse.device == self.device),
-              "locks_kvq_attend: lse is contiguous fp32 [tokens, Hq]")
-        heads = c.num_q_heads if c.combine == COMBINE_PER_HEAD else c.num_kv_heads
-        ids = self._ints(page_ids, (batch, heads, self.k), "locks_kvq_attend: page_ids")
-        cnt = self._ints(page_count, (batch, heads), "locks_kvq_attend: page_count")
-        cu = self._ints(cu_tokens, (batch + 1,), "locks_kvq_attend: cu_tokens")
-        s = kvq.struct()
-        with _Device(self.device):
-            _check(lib().locks_kvq_attend(self.handle, q.data_ptr(), cu, n, C.byref(s), batch, ids, cnt, out.data_ptr(),
-                                          None if lse is None else lse.data_ptr(), self._launch(stream)), "locks_kvq_attend")
+        self._calls.kvq_attend(self._call, q, kvq, batch, out, lse, page_ids, page_count, cu_tokens, stream)
 
     def locks_kvq_build_summaries(self, kvq: KVQView, batch, summaries, page_begin=None, page_end=None, stream=None):
         """locks_build_summaries from the codes of the 8-bit cache."""
-        self._kvq_ok(kvq, batch, "locks_kvq_build_summaries")
-        _need(summaries.dtype == torch.uint8 and summaries.is_contiguous() and summaries.device == self.device and
-              summaries.numel() >= kvq.k.shape[0] * self.cfg.num_kv_heads * self.summary_bytes, "locks_kvq_build_summaries: summaries of Context.new_summaries expected")
-        s = kvq.struct()
-        with _Device(self.device):
-            _check(lib().locks_kvq_build_summaries(self.handle, C.byref(s), batch, self._ints(page_begin, (batch,), "page_begin"),
-                                                   self._ints(page_end, (batch,), "page_end"), summaries.data_ptr(), self._launch(stream)),
-                   "locks_kvq_build_summaries")
+        self._calls.kvq_build_summaries(self._call, kvq, batch, summaries, page_begin, page_end, stream)
 
     def locks_poll_status(self, stream=None) -> int:
         st = C.c_int32(0)

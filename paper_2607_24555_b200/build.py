@@ -1,4 +1,4 @@
-"""Build liblocks.so in-tree with nvcc for sm_100a (cross-compiles without a GPU)."""
+"""Build liblocks.so in-tree with nvcc for sm_100a (cross-compiles without a GPU), and _calls.so, its native marshalling, with g++."""
 from __future__ import annotations
 
 import glob
@@ -10,6 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liblocks.so")
+CALLS = os.path.join(HERE, "_calls.so")
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-shared"]
@@ -27,7 +28,27 @@ def stale() -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def build_calls(force: bool = False) -> str:
+    import sysconfig
+
+    import torch
+    src, header = os.path.join(CSRC, "calls.cpp"), os.path.join(ROOT, "include", "locks.h")
+    if not force and os.path.exists(CALLS) and all(os.path.getmtime(f) <= os.path.getmtime(CALLS) for f in (src, header)):
+        return CALLS
+    t = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
+    inc = [os.path.join(ROOT, "include"), os.path.join(t, "include"), os.path.join(t, "include", "torch", "csrc", "api", "include"),
+           os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"] + \
+          [x for i in inc for x in ("-I", i)] + ["-o", CALLS, src, "-L", os.path.join(t, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python"]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError("g++ failed:\n" + res.stdout + res.stderr)
+    return CALLS
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
+    build_calls(force)
     if not force and not stale():
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
