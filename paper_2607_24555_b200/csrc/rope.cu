@@ -4,7 +4,7 @@
 // fp64 turns (at position 10^6 the product's rounding to fp32 would be 0.03 rad), reduced to a fraction of a turn, and only then
 // go to fp32; rows are turned in fp32 and rounded once.  A token's cosines and sines are worked out once, in shared memory, for
 // all of its heads.
-#include <mutex>
+#include <algorithm>
 
 #include "kvq.cuh"
 
@@ -62,11 +62,34 @@ __device__ __forceinline__ void unit_turn(float (&v)[16], const float2 (&cs)[8],
   }
 }
 
+// A unit's two runs as they lie in memory
+template <typename T> struct Raw {
+  static constexpr int N = sizeof(T) == 2 ? 1 : 2;   // 16-byte pieces of a run
+  uint4 w[2 * N];
+  __device__ __forceinline__ void load(const T *p, int lo, int hi) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) { w[i] = reinterpret_cast<const uint4 *>(p + lo)[i]; w[N + i] = reinterpret_cast<const uint4 *>(p + hi)[i]; }
+  }
+  __device__ __forceinline__ void store(T *p, int lo, int hi) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) { reinterpret_cast<uint4 *>(p + lo)[i] = w[i]; reinterpret_cast<uint4 *>(p + hi)[i] = w[N + i]; }
+  }
+  __device__ __forceinline__ void get(float (&v)[16]) const {
+    load8(reinterpret_cast<const T *>(&w[0]), v);
+    load8(reinterpret_cast<const T *>(&w[N]), v + 8);
+  }
+  __device__ __forceinline__ void set(const float (&v)[16]) {
+    store8(reinterpret_cast<T *>(&w[0]), v);
+    store8(reinterpret_cast<T *>(&w[N]), v + 8);
+  }
+};
+
 struct RopeParams {
   locks_rotary rot;
   const int32_t *positions, *cu;
   Rows q, qo, k, ko, v;      // ko: locks_rope only
   int n, Hq, Hk, Hv, batch;  // Hq, Hk, Hv: heads of each that this call takes (0: none)
+  int tokens;                // of a CTA
   // the cache of locks_append_rows
   char *kc, *vc;
   int64_t sb, sh, st;
@@ -75,101 +98,140 @@ struct RopeParams {
   int32_t *status;
 };
 
-// A CTA per token row: 16 heads at a time, each by eight threads of which one has a unit.  Bound by the chain of a few round trips
-// when there are few tokens (lengths and offsets; block; and rows, which are fetched meanwhile), by memory when there are many.
-constexpr int kRopeThreads = 128, kRopeAhead = 4;   // units that a thread has in flight
+// A CTA per one to eight token rows: 16 heads at a time, each by eight threads of which one has a unit, the next heads' loads under way
+// while these are turned.  Bound by the chain of a few round trips when there are few tokens (lengths and offsets; block; and rows,
+// which are fetched meanwhile), by memory when there are many.
+constexpr int kRopeThreads = 128, kRopeTokens = 8;
 
 template <typename T, bool APPEND>
 __global__ void __launch_bounds__(kRopeThreads) rope_rows_kernel(const __grid_constant__ RopeParams p) {
-  __shared__ float2 cs_s[64];
-  __shared__ int owner_s, pos_s, block_s;
-  const int tid = threadIdx.x, row = blockIdx.x, half = p.rot.rot_dim / 2, u = tid & 7;
-  const bool turns = p.rot.rot_dim > 0;
+  constexpr int kAhead = sizeof(T) == 2 ? 4 : 2;   // units that a thread fetches at a time
+  __shared__ __align__(16) float2 cs_s[kRopeTokens][64];
+  __shared__ int owner_s[kRopeTokens], pos_s[kRopeTokens], block_s[kRopeTokens];
+  const int tid = threadIdx.x, row0 = blockIdx.x * p.tokens, toks = min(p.tokens, p.n - row0), half = p.rot.rot_dim / 2, u = tid & 7, inter = p.rot.interleaved;
   float inv = 0.f;
   int axis = 0;
-  if (tid < half) { inv = p.rot.inv_freq[tid]; axis = p.rot.axis[tid]; }
+  const int f = tid & 63;   // this thread's frequency, for every other token
+  if (f < half) { inv = p.rot.inv_freq[f]; axis = p.rot.axis[f]; }
   int lo, hi;
-  unit_runs(u, p.rot.rot_dim, p.rot.interleaved, lo, hi);
+  unit_runs(u, p.rot.rot_dim, inter, lo, hi);
   const int heads = p.Hq + p.Hk + p.Hv;
+  const bool mine = u < p.rot.rot_dim / 16;
   pdl_trigger();
   pdl_wait();
-  int pos = 0, len = 0;
-  if (p.positions && tid < half) pos = p.positions[(int64_t)axis * p.n + row];
-  auto src = [&](int h) -> const T * {
-    const Rows &r = h < p.Hq ? p.q : (h < p.Hq + p.Hk ? p.k : p.v);
-    const int hh = h < p.Hq ? h : (h < p.Hq + p.Hk ? h - p.Hq : h - p.Hq - p.Hk);
-    return reinterpret_cast<const T *>(r.p) + (int64_t)row * r.st + (int64_t)hh * r.sh;
-  };
-  float x[kRopeAhead][16];
-  auto fetch = [&](int h0) {
-#pragma unroll
-    for (int i = 0; i < kRopeAhead; ++i) {
-      const int h = h0 + (tid >> 3) + 16 * i;
-      if (h < heads) {
-        const T *s = src(h);
-        load8(s + lo, x[i]);
-        load8(s + hi, x[i] + 8);
-      }
+  // head h of the CTA's token t, counted on from this thread's first by 16 heads at a time
+  struct At {
+    int t, h;
+    __device__ __forceinline__ void on(int heads) {
+      h += 16;
+      while (h >= heads) { h -= heads; ++t; }
     }
   };
+  At next = {0, tid >> 3};
+  while (next.h >= heads) { next.h -= heads; ++next.t; }
+  auto src = [&](const At &a) -> const T * {
+    const bool q = a.h < p.Hq, k = !q && a.h < p.Hq + p.Hk;
+    const Rows &r = q ? p.q : (k ? p.k : p.v);
+    const int hh = a.h - (q ? 0 : (k ? p.Hq : p.Hq + p.Hk));
+    return reinterpret_cast<const T *>(r.p) + (int64_t)(row0 + a.t) * r.st + (int64_t)hh * r.sh;
+  };
+  Raw<T> x[2][kAhead];
+  At at[2];   // of the batch's first unit
+  auto fetch = [&](Raw<T> (&y)[kAhead], At &from) {
+    from = next;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      if (next.t < toks) y[i].load(src(next), lo, hi);
+      next.on(heads);
+    }
+  };
+  int pos[kRopeTokens / 2];
+  auto place_of = [&](int t) { return p.positions ? p.positions[(int64_t)axis * p.n + row0 + t] : (APPEND ? pos_s[t] : 0); };
+  if (p.positions && f < half) {
+#pragma unroll
+    for (int i = 0; i < kRopeTokens / 2; ++i) pos[i] = (tid >> 6) + 2 * i < toks ? place_of((tid >> 6) + 2 * i) : 0;
+  }
   if (APPEND) {
-    // whose row this is: the request with cu[b] <= row < cu[b + 1]
-    if (tid == 0) owner_s = -1;
+    // whose rows these are: the request with cu[b] <= row < cu[b + 1]
+    if (tid < kRopeTokens) owner_s[tid] = -1;
     __syncthreads();
     if (!p.cu) {
-      if (tid == 0) {
-        len = p.seq_lens[row];
-        pos_s = len - 1;
-        if (len != 0) owner_s = row;   // (a length of zero: no token)
+      if (tid < toks) {
+        const int len = p.seq_lens[row0 + tid];
+        pos_s[tid] = len - 1;
+        if (len != 0) owner_s[tid] = row0 + tid;   // (a length of zero: no token)
       }
     } else {
       for (int b = tid; b < p.batch; b += kRopeThreads) {
-        const int c0 = p.cu[b], c1 = p.cu[b + 1];
-        len = p.seq_lens[b];
-        if (c0 <= row && row < c1) { owner_s = b; pos_s = (int)max((int64_t)len - c1 + row, (int64_t)-1); if (c1 - c0 > len) pos_s = -1; }
+        const int c0 = p.cu[b], c1 = p.cu[b + 1], len = p.seq_lens[b];
+        for (int t = max(c0 - row0, 0); t < min(c1 - row0, toks); ++t) {
+          owner_s[t] = b;
+          pos_s[t] = c1 - c0 > len ? -1 : (int)max((int64_t)len - c1 + row0 + t, (int64_t)-1);
+        }
       }
     }
-    fetch(0);
-    __syncthreads();
-    if (owner_s < 0) return;   // a row behind the last request's
-    if (tid == 0) {
-      const int at = pos_s, page = at < 0 ? -1 : at / p.B;
-      int block = -1;
-      if (page >= 0 && page < p.Pmax) block = p.block_table[(int64_t)owner_s * p.Pmax + page];
-      if (block < 0 || block >= p.num_blocks) { block = -1; set_status(p.status, LOCKS_ERR_BAD_BLOCK); }
-      block_s = block;
-    }
-    if (!p.positions) pos = pos_s;
-  } else {
-    fetch(0);
   }
-  if (tid < half) cs_s[tid] = turn(pos, inv);
-  __syncthreads();
-  float2 cs[8];
-  const bool mine = u < p.rot.rot_dim / 16;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) cs[i] = mine ? cs_s[8 * u + i] : make_float2(1.f, 0.f);
-  for (int h0 = 0; h0 < heads; h0 += 16 * kRopeAhead) {
-    if (h0) fetch(h0);
-#pragma unroll
-    for (int i = 0; i < kRopeAhead; ++i) {
-      const int h = h0 + (tid >> 3) + 16 * i;
-      if (h >= heads) break;
-      if (turns && mine && h < p.Hq + p.Hk) unit_turn(x[i], cs, p.rot.interleaved);
-      T *d;
-      if (h < p.Hq) {
-        d = reinterpret_cast<T *>(const_cast<char *>(p.qo.p)) + (int64_t)row * p.qo.st + (int64_t)h * p.qo.sh;
-      } else if (!APPEND) {
-        d = reinterpret_cast<T *>(const_cast<char *>(p.ko.p)) + (int64_t)row * p.ko.st + (int64_t)(h - p.Hq) * p.ko.sh;
-      } else {
-        if (block_s < 0) continue;
-        const bool key = h < p.Hq + p.Hk;
-        const int hh = h - p.Hq - (key ? 0 : p.Hk);
-        d = reinterpret_cast<T *>(key ? p.kc : p.vc) + (int64_t)block_s * p.sb + (int64_t)hh * p.sh + (int64_t)(pos_s % p.B) * p.st;
+  fetch(x[0], at[0]);
+  if (APPEND) {
+    __syncthreads();
+    if (tid < toks) {
+      int block = -1;
+      if (owner_s[tid] >= 0) {   // (else a row behind the last request's)
+        const int place = pos_s[tid], page = place < 0 ? -1 : place / p.B;
+        if (page >= 0 && page < p.Pmax) block = p.block_table[(int64_t)owner_s[tid] * p.Pmax + page];
+        if (block < 0 || block >= p.num_blocks) { block = -1; set_status(p.status, LOCKS_ERR_BAD_BLOCK); }
       }
-      store8(d + lo, x[i]);
-      store8(d + hi, x[i] + 8);
+      block_s[tid] = block;
     }
+    if (!p.positions && f < half) {
+#pragma unroll
+      for (int i = 0; i < kRopeTokens / 2; ++i) pos[i] = (tid >> 6) + 2 * i < toks ? place_of((tid >> 6) + 2 * i) : 0;
+    }
+  }
+  if (f < half) {
+#pragma unroll
+    for (int i = 0; i < kRopeTokens / 2; ++i)
+      if ((tid >> 6) + 2 * i < toks) cs_s[(tid >> 6) + 2 * i][f] = turn(pos[i], inv);
+  }
+  __syncthreads();
+  auto give = [&](Raw<T> (&y)[kAhead], At a) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i, a.on(heads)) {
+      if (a.t >= toks) break;
+      if (APPEND && owner_s[a.t] < 0) continue;
+      T *d;
+      if (a.h < p.Hq) {
+        d = reinterpret_cast<T *>(const_cast<char *>(p.qo.p)) + (int64_t)(row0 + a.t) * p.qo.st + (int64_t)a.h * p.qo.sh;
+      } else if (!APPEND) {
+        d = reinterpret_cast<T *>(const_cast<char *>(p.ko.p)) + (int64_t)(row0 + a.t) * p.ko.st + (int64_t)(a.h - p.Hq) * p.ko.sh;
+      } else {
+        if (block_s[a.t] < 0) continue;
+        const bool key = a.h < p.Hq + p.Hk;
+        const int hh = a.h - p.Hq - (key ? 0 : p.Hk);
+        d = reinterpret_cast<T *>(key ? p.kc : p.vc) + (int64_t)block_s[a.t] * p.sb + (int64_t)hh * p.sh + (int64_t)(pos_s[a.t] % p.B) * p.st;
+      }
+      if (mine && a.h < p.Hq + p.Hk) {
+        float v[16];
+        float2 cs[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float4 c2 = reinterpret_cast<const float4 *>(&cs_s[a.t][8 * u])[e];
+          cs[2 * e] = make_float2(c2.x, c2.y);
+          cs[2 * e + 1] = make_float2(c2.z, c2.w);
+        }
+        y[i].get(v);
+        unit_turn(v, cs, inter);
+        y[i].set(v);
+      }
+      y[i].store(d, lo, hi);
+    }
+  };
+  while (at[0].t < toks) {
+    fetch(x[1], at[1]);
+    give(x[0], at[0]);
+    if (at[1].t >= toks) break;
+    fetch(x[0], at[0]);
+    give(x[1], at[1]);
   }
 }
 
@@ -206,7 +268,7 @@ template <int FMT> __device__ __forceinline__ uint32_t code4(const float *v, flo
 // all heads, and the query rows of its tokens.
 template <int FMT>
 __global__ void __launch_bounds__(kQThreads) kvq_append_kernel(const __grid_constant__ QAppendParams p) {
-  extern __shared__ float2 cs_s[];   // [B][64]
+  extern __shared__ __align__(16) float2 cs_s[];   // [B][64]
   __shared__ int found_s[4];         // request, item of it, first row, new tokens
   __shared__ int warp_s[kQWarps];
   __shared__ uint32_t amax_s[kQWarps];
@@ -285,7 +347,11 @@ __global__ void __launch_bounds__(kQThreads) kvq_append_kernel(const __grid_cons
     auto turned = [&](float (&x)[16], int t) {   // t: token of this page's new ones
       float2 cs[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) cs[i] = cs_s[t * 64 + 8 * u + i];
+      for (int e = 0; e < 4; ++e) {
+        const float4 c2 = reinterpret_cast<const float4 *>(cs_s + t * 64 + 8 * u)[e];
+        cs[2 * e] = make_float2(c2.x, c2.y);
+        cs[2 * e + 1] = make_float2(c2.z, c2.w);
+      }
       unit_turn(x, cs, inter);
     };
     // ---- keys and values
@@ -354,20 +420,29 @@ __global__ void __launch_bounds__(kQThreads) kvq_append_kernel(const __grid_cons
         }
       }
     }
-    // ---- query rows of the page's new tokens
+    // ---- query rows of the page's new tokens, four of a thread's at a time
     if (p.qo.p) {
+      constexpr int kAhead = 4;
       const int rows = (t1 - t0) * p.Hq;
-      for (int r = tid >> 3; r < rows; r += kQThreads / 8) {
-        const int t = r / p.Hq, h = r - t * p.Hq;
-        const int64_t row = row0 + t0 + t - start;
-        const __nv_bfloat16 *s = reinterpret_cast<const __nv_bfloat16 *>(p.q.p) + row * p.q.st + (int64_t)h * p.q.sh;
-        __nv_bfloat16 *d = reinterpret_cast<__nv_bfloat16 *>(const_cast<char *>(p.qo.p)) + row * p.qo.st + (int64_t)h * p.qo.sh;
-        float x[16];
-        load8(s + lo, x);
-        load8(s + hi, x + 8);
-        if (mine) turned(x, t);
-        store8(d + lo, x);
-        store8(d + hi, x + 8);
+      for (int r0 = tid >> 3; r0 < rows; r0 += kAhead * kQThreads / 8) {
+        Raw<__nv_bfloat16> y[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+          const int r = r0 + i * kQThreads / 8, t = r / p.Hq, h = r - t * p.Hq;
+          if (r < rows) y[i].load(reinterpret_cast<const __nv_bfloat16 *>(p.q.p) + (int64_t)(row0 + t0 + t - start) * p.q.st + (int64_t)h * p.q.sh, lo, hi);
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+          const int r = r0 + i * kQThreads / 8, t = r / p.Hq, h = r - t * p.Hq;
+          if (r >= rows) break;
+          if (mine) {
+            float x[16];
+            y[i].get(x);
+            turned(x, t);
+            y[i].set(x);
+          }
+          y[i].store(reinterpret_cast<__nv_bfloat16 *>(const_cast<char *>(p.qo.p)) + (int64_t)(row0 + t0 + t - start) * p.qo.st + (int64_t)h * p.qo.sh, lo, hi);
+        }
       }
     }
   };
@@ -405,6 +480,15 @@ int append_ok(const locks_ctx *c, const locks_rotary *rot, const int32_t *cu, in
   return rot ? rotary_ok(rot) : LOCKS_OK;
 }
 
+// Token rows a CTA: one while there are CTAs to spare, up to eight (a token's chain of lengths, block and angles is then paid once for
+// several)
+template <bool APPEND> void launch_rows(locks_ctx *c, RopeParams &p, cudaStream_t st) {
+  p.tokens = std::min(std::max(p.n / (4 * c->num_sms), 1), kRopeTokens);
+  const dim3 grid((p.n - 1) / p.tokens + 1);
+  if (c->cfg.kv_dtype == LOCKS_BF16) locks_launch_pdl(rope_rows_kernel<__nv_bfloat16, APPEND>, grid, dim3(kRopeThreads), 0, st, p);
+  else locks_launch_pdl(rope_rows_kernel<float, APPEND>, grid, dim3(kRopeThreads), 0, st, p);
+}
+
 }  // namespace
 
 extern "C" int locks_rope(locks_ctx *ctx, const locks_rotary *rot, const int32_t *positions, int num_tokens, const locks_rows *q,
@@ -420,8 +504,7 @@ extern "C" int locks_rope(locks_ctx *ctx, const locks_rotary *rot, const int32_t
   p.q = rows(q); p.qo = rows(q_out); p.k = rows(k); p.ko = rows(k_out);
   p.Hq = q ? ctx->cfg.num_q_heads : 0; p.Hk = k ? ctx->cfg.num_kv_heads : 0;
   ctx->last_launches = 0;
-  if (ctx->cfg.kv_dtype == LOCKS_BF16) locks_launch_pdl(rope_rows_kernel<__nv_bfloat16, false>, dim3(num_tokens), dim3(kRopeThreads), 0, (cudaStream_t)stream, p);
-  else locks_launch_pdl(rope_rows_kernel<float, false>, dim3(num_tokens), dim3(kRopeThreads), 0, (cudaStream_t)stream, p);
+  launch_rows<false>(ctx, p, (cudaStream_t)stream);
   return locks_check_launch(ctx);
 }
 
@@ -445,8 +528,7 @@ extern "C" int locks_append_rows(locks_ctx *ctx, const locks_rotary *rot, const 
   p.block_table = kv->block_table; p.seq_lens = kv->seq_lens; p.num_blocks = kv->num_blocks; p.Pmax = ctx->Pmax; p.B = ctx->B;
   p.status = ctx->status;
   ctx->last_launches = 0;
-  if (ctx->cfg.kv_dtype == LOCKS_BF16) locks_launch_pdl(rope_rows_kernel<__nv_bfloat16, true>, dim3(num_tokens), dim3(kRopeThreads), 0, (cudaStream_t)stream, p);
-  else locks_launch_pdl(rope_rows_kernel<float, true>, dim3(num_tokens), dim3(kRopeThreads), 0, (cudaStream_t)stream, p);
+  launch_rows<true>(ctx, p, (cudaStream_t)stream);
   return locks_check_launch(ctx);
 }
 
