@@ -51,6 +51,17 @@ __device__ __forceinline__ void unit_runs(int u, int rot, int inter, int &lo, in
   if (inter || u >= rot / 16) { lo = 16 * u; hi = lo + 8; }
   else { lo = 8 * u; hi = rot / 2 + lo; }
 }
+// A token's cosines and sines lie such that the eight units of a head read 16 bytes each side by side: pair f = 8 u + 2 e + c of the
+// token at 16 e + 2 u + c.
+__device__ __forceinline__ int turn_at(int f) { return 16 * ((f >> 1) & 3) + 2 * (f >> 3) + (f & 1); }
+__device__ __forceinline__ void unit_turns(const float2 *token, int u, float2 (&cs)[8]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float4 c = reinterpret_cast<const float4 *>(token)[8 * e + u];
+    cs[2 * e] = make_float2(c.x, c.y);
+    cs[2 * e + 1] = make_float2(c.z, c.w);
+  }
+}
 // v: the runs' values, cs: cosines and sines of the unit's pairs
 __device__ __forceinline__ void unit_turn(float (&v)[16], const float2 (&cs)[8], int inter) {
 #pragma unroll
@@ -98,58 +109,50 @@ struct RopeParams {
   int32_t *status;
 };
 
-// A CTA per one to eight token rows: 16 heads at a time, each by eight threads of which one has a unit, the next heads' loads under way
-// while these are turned.  Bound by the chain of a few round trips when there are few tokens (lengths and offsets; block; and rows,
-// which are fetched meanwhile), by memory when there are many.
-constexpr int kRopeThreads = 128, kRopeTokens = 8;
+// A CTA of NT threads takes one token row (ONE), or up to kRopeTokens: NT / 8 heads at a time, each by eight threads of which one has a
+// unit.  A thread fetches four units at a time, of four tokens (ONE: of four of its heads), while it turns the four before.  Bound by
+// the chain of a few round trips when there are few tokens (lengths and offsets; block; and rows, which are fetched meanwhile), by
+// memory when there are many.
+constexpr int kRopeThreads = 128, kRopeTokens = 8, kAhead = 4;
 
-template <typename T, bool APPEND>
-__global__ void __launch_bounds__(kRopeThreads) rope_rows_kernel(const __grid_constant__ RopeParams p) {
-  constexpr int kAhead = sizeof(T) == 2 ? 4 : 2;   // units that a thread fetches at a time
+template <typename T, bool APPEND, bool ONE, int NT>
+__device__ __forceinline__ void rope_rows(const RopeParams &p, int cta) {
   __shared__ __align__(16) float2 cs_s[kRopeTokens][64];
-  __shared__ int owner_s[kRopeTokens], pos_s[kRopeTokens], block_s[kRopeTokens];
-  const int tid = threadIdx.x, row0 = blockIdx.x * p.tokens, toks = min(p.tokens, p.n - row0), half = p.rot.rot_dim / 2, u = tid & 7, inter = p.rot.interleaved;
+  __shared__ int owner_s[kRopeTokens], pos_s[kRopeTokens];
+  __shared__ int64_t at_s[kRopeTokens];   // the token's row in the cache (elements), or -1
+  const int tid = threadIdx.x, row0 = cta * p.tokens, toks = ONE ? 1 : min(p.tokens, p.n - row0), half = p.rot.rot_dim / 2, u = tid & 7, inter = p.rot.interleaved;
+  constexpr int kEach = NT / 64, kTurns = ONE ? 1 : (kRopeTokens + kEach - 1) / kEach;
+  const int f = tid & 63, t0 = tid >> 6;   // this thread's frequency, for tokens t0, t0 + kEach, ..
   float inv = 0.f;
   int axis = 0;
-  const int f = tid & 63;   // this thread's frequency, for every other token
   if (f < half) { inv = p.rot.inv_freq[f]; axis = p.rot.axis[f]; }
   int lo, hi;
   unit_runs(u, p.rot.rot_dim, inter, lo, hi);
-  const int heads = p.Hq + p.Hk + p.Hv;
+  const int heads = p.Hq + p.Hk + p.Hv, hi_off = hi - lo;
   const bool mine = u < p.rot.rot_dim / 16;
-  pdl_trigger();
-  pdl_wait();
-  // head h of the CTA's token t, counted on from this thread's first by 16 heads at a time
-  struct At {
-    int t, h;
-    __device__ __forceinline__ void on(int heads) {
-      h += 16;
-      while (h >= heads) { h -= heads; ++t; }
-    }
-  };
-  At next = {0, tid >> 3};
-  while (next.h >= heads) { next.h -= heads; ++next.t; }
-  auto src = [&](const At &a) -> const T * {
-    const bool q = a.h < p.Hq, k = !q && a.h < p.Hq + p.Hk;
-    const Rows &r = q ? p.q : (k ? p.k : p.v);
-    const int hh = a.h - (q ? 0 : (k ? p.Hq : p.Hq + p.Hk));
-    return reinterpret_cast<const T *>(r.p) + (int64_t)(row0 + a.t) * r.st + (int64_t)hh * r.sh;
+  // units in batches of kAhead: ONE: heads (tid >> 3) + NT / 8 (k + i) of the token; else head (tid >> 3) + NT / 8 (k / kRopeTokens), tokens k % kRopeTokens + i
+  const int passes = (heads + NT / 8 - 1) / (NT / 8), end = ONE ? passes : passes * kRopeTokens;
+  auto head_of = [&](int k, int i) { return (tid >> 3) + NT / 8 * (ONE ? k + i : k / kRopeTokens); };
+  auto token_of = [&](int k, int i) { return ONE ? 0 : k % kRopeTokens + i; };
+  struct Line { const char *p; int64_t st; };   // a head's row of the CTA's first token (values are chosen: a reference chosen would be fetched lane by lane)
+  auto source = [&](int h) {
+    const bool q = h < p.Hq, k = !q && h < p.Hq + p.Hk;
+    const int64_t st = q ? p.q.st : (k ? p.k.st : p.v.st), sh = q ? p.q.sh : (k ? p.k.sh : p.v.sh);
+    return Line{(q ? p.q.p : (k ? p.k.p : p.v.p)) + (row0 * st + (h - (q ? 0 : (k ? p.Hq : p.Hq + p.Hk))) * sh + lo) * (int64_t)sizeof(T), st * (int64_t)sizeof(T)};
   };
   Raw<T> x[2][kAhead];
-  At at[2];   // of the batch's first unit
-  auto fetch = [&](Raw<T> (&y)[kAhead], At &from) {
-    from = next;
+  auto fetch = [&](Raw<T> (&y)[kAhead], int k) {
+    Line l = source(head_of(k, 0));
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
-      if (next.t < toks) y[i].load(src(next), lo, hi);
-      next.on(heads);
+      if (ONE && i) l = source(head_of(k, i));
+      if (k < end && head_of(k, i) < heads && token_of(k, i) < toks) y[i].load(reinterpret_cast<const T *>(l.p + token_of(k, i) * l.st), 0, hi_off);
     }
   };
-  int pos[kRopeTokens / 2];
-  auto place_of = [&](int t) { return p.positions ? p.positions[(int64_t)axis * p.n + row0 + t] : (APPEND ? pos_s[t] : 0); };
+  int pos[kTurns];
   if (p.positions && f < half) {
 #pragma unroll
-    for (int i = 0; i < kRopeTokens / 2; ++i) pos[i] = (tid >> 6) + 2 * i < toks ? place_of((tid >> 6) + 2 * i) : 0;
+    for (int i = 0; i < kTurns; ++i) pos[i] = t0 + kEach * i < toks ? p.positions[(int64_t)axis * p.n + row0 + t0 + kEach * i] : 0;
   }
   if (APPEND) {
     // whose rows these are: the request with cu[b] <= row < cu[b + 1]
@@ -162,7 +165,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_rows_kernel(const __grid_co
         if (len != 0) owner_s[tid] = row0 + tid;   // (a length of zero: no token)
       }
     } else {
-      for (int b = tid; b < p.batch; b += kRopeThreads) {
+      for (int b = tid; b < p.batch; b += NT) {
         const int c0 = p.cu[b], c1 = p.cu[b + 1], len = p.seq_lens[b];
         for (int t = max(c0 - row0, 0); t < min(c1 - row0, toks); ++t) {
           owner_s[t] = b;
@@ -171,76 +174,75 @@ __global__ void __launch_bounds__(kRopeThreads) rope_rows_kernel(const __grid_co
       }
     }
   }
-  fetch(x[0], at[0]);
+  fetch(x[0], 0);
   if (APPEND) {
     __syncthreads();
     if (tid < toks) {
-      int block = -1;
-      if (owner_s[tid] >= 0) {   // (else a row behind the last request's)
+      int64_t at = -1;
+      if (owner_s[tid] >= 0 && p.Hk) {   // (else a row behind the last request's)
         const int place = pos_s[tid], page = place < 0 ? -1 : place / p.B;
+        int block = -1;
         if (page >= 0 && page < p.Pmax) block = p.block_table[(int64_t)owner_s[tid] * p.Pmax + page];
-        if (block < 0 || block >= p.num_blocks) { block = -1; set_status(p.status, LOCKS_ERR_BAD_BLOCK); }
+        if (block >= 0 && block < p.num_blocks) at = (int64_t)block * p.sb + (int64_t)(place - page * p.B) * p.st;
+        else set_status(p.status, LOCKS_ERR_BAD_BLOCK);
       }
-      block_s[tid] = block;
+      at_s[tid] = at;
     }
     if (!p.positions && f < half) {
 #pragma unroll
-      for (int i = 0; i < kRopeTokens / 2; ++i) pos[i] = (tid >> 6) + 2 * i < toks ? place_of((tid >> 6) + 2 * i) : 0;
+      for (int i = 0; i < kTurns; ++i) pos[i] = t0 + kEach * i < toks ? pos_s[t0 + kEach * i] : 0;
     }
   }
   if (f < half) {
 #pragma unroll
-    for (int i = 0; i < kRopeTokens / 2; ++i)
-      if ((tid >> 6) + 2 * i < toks) cs_s[(tid >> 6) + 2 * i][f] = turn(pos[i], inv);
+    for (int i = 0; i < kTurns; ++i)
+      if (t0 + kEach * i < toks) cs_s[t0 + kEach * i][turn_at(f)] = turn(pos[i], inv);
   }
   __syncthreads();
-  auto give = [&](Raw<T> (&y)[kAhead], At a) {
+  auto give = [&](Raw<T> (&y)[kAhead], int k) {
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i, a.on(heads)) {
-      if (a.t >= toks) break;
-      if (APPEND && owner_s[a.t] < 0) continue;
-      T *d;
-      if (a.h < p.Hq) {
-        d = reinterpret_cast<T *>(const_cast<char *>(p.qo.p)) + (int64_t)(row0 + a.t) * p.qo.st + (int64_t)a.h * p.qo.sh;
-      } else if (!APPEND) {
-        d = reinterpret_cast<T *>(const_cast<char *>(p.ko.p)) + (int64_t)(row0 + a.t) * p.ko.st + (int64_t)(a.h - p.Hq) * p.ko.sh;
-      } else {
-        if (block_s[a.t] < 0) continue;
-        const bool key = a.h < p.Hq + p.Hk;
-        const int hh = a.h - p.Hq - (key ? 0 : p.Hk);
-        d = reinterpret_cast<T *>(key ? p.kc : p.vc) + (int64_t)block_s[a.t] * p.sb + (int64_t)hh * p.sh + (int64_t)(pos_s[a.t] % p.B) * p.st;
-      }
-      if (mine && a.h < p.Hq + p.Hk) {
+    for (int i = 0; i < kAhead; ++i) {
+      const int h = head_of(k, i), t = token_of(k, i);
+      if (h >= heads || t >= toks || (APPEND && owner_s[t] < 0)) continue;
+      const bool q = h < p.Hq, key = h < p.Hq + p.Hk;
+      if (mine && key) {
         float v[16];
         float2 cs[8];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float4 c2 = reinterpret_cast<const float4 *>(&cs_s[a.t][8 * u])[e];
-          cs[2 * e] = make_float2(c2.x, c2.y);
-          cs[2 * e + 1] = make_float2(c2.z, c2.w);
-        }
         y[i].get(v);
+        unit_turns(cs_s[t], u, cs);
         unit_turn(v, cs, inter);
         y[i].set(v);
       }
-      y[i].store(d, lo, hi);
+      T *d;
+      if (q || !APPEND) {
+        d = reinterpret_cast<T *>(const_cast<char *>(q ? p.qo.p : p.ko.p)) + (int64_t)(row0 + t) * (q ? p.qo.st : p.ko.st) + (h - (q ? 0 : p.Hq)) * (q ? p.qo.sh : p.ko.sh);
+      } else {
+        if (at_s[t] < 0) continue;
+        d = reinterpret_cast<T *>(key ? p.kc : p.vc) + at_s[t] + (h - p.Hq - (key ? 0 : p.Hk)) * p.sh;
+      }
+      y[i].store(d + lo, 0, hi_off);
     }
   };
-  while (at[0].t < toks) {
-    fetch(x[1], at[1]);
-    give(x[0], at[0]);
-    if (at[1].t >= toks) break;
-    fetch(x[0], at[0]);
-    give(x[1], at[1]);
+#pragma unroll 1
+  for (int k = 0; k < end; k += 2 * kAhead) {
+    fetch(x[1], k + kAhead);
+    give(x[0], k);
+    fetch(x[0], k + 2 * kAhead);
+    if (k + kAhead < end) give(x[1], k + kAhead);
   }
+}
+
+template <typename T, bool APPEND, bool ONE>
+__global__ void __launch_bounds__(kRopeThreads) rope_rows_kernel(const __grid_constant__ RopeParams p) {
+  pdl_trigger();
+  pdl_wait();
+  rope_rows<T, APPEND, ONE, kRopeThreads>(p, blockIdx.x);
 }
 
 // ------------------------------------------------------------------------------------------------ the 8-bit cache
 struct QAppendParams {
-  locks_rotary rot;
-  const int32_t *positions, *cu;
-  Rows q, qo, k, v;
-  int n, Hq, batch;
+  RopeParams r;    // rotation, positions, offsets, rows; its Hq heads of queries alone
+  int q_ctas;      // the first CTAs take the query rows
   KvqCache c;
   int32_t *status;
 };
@@ -248,38 +250,55 @@ struct QAppendParams {
 constexpr int kMostTokens = 1 << 30;   // places stay far from 32 bits' end
 constexpr int kQWarps = 8, kQThreads = kQWarps * 32;
 
-template <int FMT> __device__ __forceinline__ uint32_t code4(const float *v, float scale) {   // true quotients, rounded to even
-  if (FMT == LOCKS_KVQ_INT) {
-    int c[4];
+// x / scale, rounded to nearest: the product with the rounded reciprocal, and one correction by the remainder (Markstein 1990), which
+// a multiply-add gives exactly
+__device__ __forceinline__ float quotient(float x, float scale, float inv) {
+  const float q = x * inv;
+  return fmaf(fmaf(-q, scale, x), inv, q);
+}
+template <int FMT> __device__ __forceinline__ uint32_t code4(const float *v, float scale, float inv) {   // rounded to even
+  float q[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) c[i] = __float2int_rn(fminf(fmaxf(__fdiv_rn(v[i], scale), -127.f), 127.f));
-    return (uint32_t)(c[0] & 255) | (uint32_t)(c[1] & 255) << 8 | (uint32_t)(c[2] & 255) << 16 | (uint32_t)(c[3] & 255) << 24;
+  for (int i = 0; i < 4; ++i) q[i] = quotient(v[i], scale, inv);
+  if (FMT == LOCKS_KVQ_INT) {   // (at most 127 and a rounding)
+    uint32_t c[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c[i] = (uint32_t)__float2int_rn(q[i]);
+    return __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
   }
   uint16_t lo, hi;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(__fdiv_rn(v[1], scale)), "f"(__fdiv_rn(v[0], scale)));
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(__fdiv_rn(v[3], scale)), "f"(__fdiv_rn(v[2], scale)));
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(q[1]), "f"(q[0]));
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(q[3]), "f"(q[2]));
   return (uint32_t)lo | (uint32_t)hi << 16;
 }
 
-// A CTA per (request, page that gets tokens and is complete afterwards), all KV heads; the first of a request's also takes its
-// unfinished last page, whose tokens replace the tail that the first page has been put together from.  A warp has 16 tokens of a
+// Query rows, and a CTA per (request, page that gets tokens and is complete afterwards), all KV heads; the first of a request's also takes
+// its unfinished last page, whose tokens replace the tail that the first page has been put together from.  A warp has 16 tokens of a
 // head's keys or values in registers (a lane: a unit of four tokens), so that the largest magnitude is known before a code is
-// written and everything is read once; pages of 32 and 64 tokens are two and four warps' work.  The CTA's cosines and sines serve
-// all heads, and the query rows of its tokens.
+// written and everything is read once; pages of 32 and 64 tokens are two and four warps'
+// work.  The CTA's cosines and sines serve all heads.
 template <int FMT>
-__global__ void __launch_bounds__(kQThreads) kvq_append_kernel(const __grid_constant__ QAppendParams p) {
+__global__ void __launch_bounds__(kQThreads, 2) kvq_append_kernel(const __grid_constant__ QAppendParams a) {
   extern __shared__ __align__(16) float2 cs_s[];   // [B][64]
   __shared__ int found_s[4];         // request, item of it, first row, new tokens
   __shared__ int warp_s[kQWarps];
   __shared__ uint32_t amax_s[kQWarps];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, B = p.c.B;
+  pdl_trigger();
+  pdl_wait();
+  const RopeParams &p = a.r;
+  if ((int)blockIdx.x < a.q_ctas) {
+    if (p.tokens == 1) rope_rows<__nv_bfloat16, true, true, kQThreads>(p, blockIdx.x);
+    else rope_rows<__nv_bfloat16, true, false, kQThreads>(p, blockIdx.x);
+    return;
+  }
+  const KvqCache &c = a.c;
+  const int cta = blockIdx.x - a.q_ctas, ctas = gridDim.x - a.q_ctas;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, B = c.B;
   const int half = p.rot.rot_dim / 2, u = lane & 7, inter = p.rot.interleaved;
   int lo, hi;
   unit_runs(u, p.rot.rot_dim, inter, lo, hi);
   const bool mine = u < p.rot.rot_dim / 16;
-  pdl_trigger();
-  pdl_wait();
-  int b = blockIdx.x, item = 0, row0 = b, n = 1;
+  int b = cta, item = 0, row0 = b, n = 1;
   if (p.cu) {
     // the request that this CTA's item belongs to: a running sum of the requests' items
     if (tid == 0) found_s[0] = -1;
@@ -290,9 +309,9 @@ __global__ void __launch_bounds__(kQThreads) kvq_append_kernel(const __grid_cons
       if (i < p.batch) {
         c0 = p.cu[i];
         m = p.cu[i + 1] - c0;
-        const int T = p.c.seq_lens[i];
+        const int T = c.seq_lens[i];
         if (m != 0 && (m < 0 || m > T || T > kMostTokens || c0 < 0 || c0 > p.n - m)) {
-          set_status(p.status, LOCKS_ERR_BAD_BLOCK);
+          set_status(a.status, LOCKS_ERR_BAD_BLOCK);
           m = 0;
         }
         if (m > 0) items = max(1, T / B - (T - m) / B);
@@ -311,18 +330,18 @@ __global__ void __launch_bounds__(kQThreads) kvq_append_kernel(const __grid_cons
         if (w < warp) sum += warp_s[w];
         all += warp_s[w];
       }
-      const int at = (int)blockIdx.x - before - (sum - items);
+      const int at = cta - before - (sum - items);
       if (at >= 0 && at < items) { found_s[0] = i; found_s[1] = at; found_s[2] = c0; found_s[3] = m; }
       before += all;
       __syncthreads();
-      if (before > (int)blockIdx.x && blockIdx.x + 1 < gridDim.x) break;   // (the last CTA looks at every request)
+      if (before > cta && cta + 1 < ctas) break;   // (the last CTA looks at every request)
     }
     if (found_s[0] < 0) return;
     b = found_s[0]; item = found_s[1]; row0 = found_s[2]; n = found_s[3];
   }
-  const int T = p.c.seq_lens[b], start = T - n;
+  const int T = c.seq_lens[b], start = T - n;
   if (start < 0 || T > kMostTokens) {   // (one token per request: none at a length of zero)
-    if (tid == 0 && T != 0) set_status(p.status, LOCKS_ERR_BAD_BLOCK);
+    if (tid == 0 && T != 0) set_status(a.status, LOCKS_ERR_BAD_BLOCK);
     return;
   }
   const int sub_shift = B == 64 ? 2 : (B == 32 ? 1 : 0);   // a page is 2^sub_shift warps' work
@@ -331,55 +350,50 @@ __global__ void __launch_bounds__(kQThreads) kvq_append_kernel(const __grid_cons
     const bool complete = first + B <= T;
     for (int i = tid; i < (t1 - t0) * half; i += kQThreads) {
       const int t = i / half, f = i - t * half, row = row0 + t0 + t - start;
-      cs_s[t * 64 + f] = turn(p.positions ? p.positions[(int64_t)p.rot.axis[f] * p.n + row] : t0 + t, p.rot.inv_freq[f]);
+      cs_s[t * 64 + turn_at(f)] = turn(p.positions ? p.positions[(int64_t)p.rot.axis[f] * p.n + row] : t0 + t, p.rot.inv_freq[f]);
     }
     int block = -1;
     if (complete) {
-      if (page < p.c.Pmax) block = p.c.block_table[(int64_t)b * p.c.Pmax + page];
-      if (block < 0 || block >= p.c.num_blocks) {
+      if (page < c.Pmax) block = c.block_table[(int64_t)b * c.Pmax + page];
+      if (block < 0 || block >= c.num_blocks) {
         block = -1;
-        if (tid == 0) set_status(p.status, LOCKS_ERR_BAD_BLOCK);
+        if (tid == 0) set_status(a.status, LOCKS_ERR_BAD_BLOCK);
       }
     }
-    const bool fits = page < p.c.Pmax;
-    if (!fits && !complete && tid == 0) set_status(p.status, LOCKS_ERR_BAD_BLOCK);
-    __syncthreads();
+    const bool fits = page < c.Pmax;
+    if (!fits && !complete && tid == 0) set_status(a.status, LOCKS_ERR_BAD_BLOCK);
     auto turned = [&](float (&x)[16], int t) {   // t: token of this page's new ones
       float2 cs[8];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float4 c2 = reinterpret_cast<const float4 *>(cs_s + t * 64 + 8 * u)[e];
-        cs[2 * e] = make_float2(c2.x, c2.y);
-        cs[2 * e + 1] = make_float2(c2.z, c2.w);
-      }
+      unit_turns(cs_s + t * 64, u, cs);
       unit_turn(x, cs, inter);
     };
     // ---- keys and values
-    const int tasks = 2 * p.c.Hkv, per_round = kQWarps >> sub_shift, sub = warp & ((1 << sub_shift) - 1);
+    const int tasks = 2 * c.Hkv, per_round = kQWarps >> sub_shift, sub = warp & ((1 << sub_shift) - 1), at0 = first + 16 * sub + (lane >> 3);
+    __syncthreads();   // the cosines are there
     for (int r = 0; r < tasks; r += per_round) {
       const int task = r + (warp >> sub_shift), h = task >> 1;
       const bool live = task < tasks, key = !(task & 1);
-      const int64_t tail0 = ((int64_t)b * p.c.Hkv + h) * B;
-      float *tail = (key ? p.c.kt : p.c.vt) + tail0 * LOCKS_D;
-      const Rows &src = key ? p.k : p.v;
+      float *tail = (key ? c.kt : c.vt) + (((int64_t)b * c.Hkv + h) * B) * LOCKS_D;
       float x[4][16];
       uint32_t amax = 0;
       if (live) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int pos = first + 16 * sub + 4 * i + (lane >> 3);
+          const int pos = at0 + 4 * i;
           if (pos < t0) {
             if (complete) { load8(tail + (pos - first) * LOCKS_D + lo, x[i]); load8(tail + (pos - first) * LOCKS_D + hi, x[i] + 8); }
           } else if (pos < t1) {
-            const __nv_bfloat16 *s = reinterpret_cast<const __nv_bfloat16 *>(src.p) + (int64_t)(row0 + pos - start) * src.st + (int64_t)h * src.sh;
+            const __nv_bfloat16 *s = reinterpret_cast<const __nv_bfloat16 *>(key ? p.k.p : p.v.p) + (int64_t)(row0 + pos - start) * (key ? p.k.st : p.v.st) + (int64_t)h * (key ? p.k.sh : p.v.sh);
             load8(s + lo, x[i]);
             load8(s + hi, x[i] + 8);
           }
         }
+      }
+      if (live && key && mine) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int pos = first + 16 * sub + 4 * i + (lane >> 3);
-          if (key && mine && pos >= t0 && pos < t1) turned(x[i], pos - t0);
+          const int pos = at0 + 4 * i;
+          if (pos >= t0 && pos < t1) turned(x[i], pos - t0);
         }
       }
       if (complete) {
@@ -401,47 +415,23 @@ __global__ void __launch_bounds__(kQThreads) kvq_append_kernel(const __grid_cons
           float scale = __fdiv_rn(__uint_as_float(amax), FMT == LOCKS_KVQ_INT ? 127.f : 448.f);
           const bool codes = amax >= KVQ_TINY_BITS && amax < 0x7f800000u;
           if (!codes) scale = amax < KVQ_TINY_BITS ? 0.f : __uint_as_float(0x7fffffffu);
-          char *dst = (key ? p.c.k : p.c.v) + (int64_t)block * p.c.sb + (int64_t)h * p.c.sh;
+          const float inv = 1.f / scale;
+          char *dst = (key ? c.k : c.v) + (int64_t)block * c.sb + (int64_t)h * c.sh;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            char *d = dst + (int64_t)(16 * sub + 4 * i + (lane >> 3)) * p.c.st;
-            const uint2 a = codes ? make_uint2(code4<FMT>(x[i], scale), code4<FMT>(x[i] + 4, scale)) : make_uint2(0, 0);
-            const uint2 c = codes ? make_uint2(code4<FMT>(x[i] + 8, scale), code4<FMT>(x[i] + 12, scale)) : make_uint2(0, 0);
+            char *d = dst + (int64_t)(16 * sub + 4 * i + (lane >> 3)) * c.st;
+            const uint2 a = codes ? make_uint2(code4<FMT>(x[i], scale, inv), code4<FMT>(x[i] + 4, scale, inv)) : make_uint2(0, 0);
+            const uint2 c = codes ? make_uint2(code4<FMT>(x[i] + 8, scale, inv), code4<FMT>(x[i] + 12, scale, inv)) : make_uint2(0, 0);
             *reinterpret_cast<uint2 *>(d + lo) = a;
             *reinterpret_cast<uint2 *>(d + hi) = c;
           }
-          if (lane == 0 && sub == 0) (key ? p.c.ks : p.c.vs)[(int64_t)block * p.c.Hkv + h] = scale;
+          if (lane == 0 && sub == 0) (key ? c.ks : c.vs)[(int64_t)block * c.Hkv + h] = scale;
         }
       } else if (live && fits) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int pos = first + 16 * sub + 4 * i + (lane >> 3);
+          const int pos = at0 + 4 * i;
           if (pos >= t0 && pos < t1) { store8(tail + (pos - first) * LOCKS_D + lo, x[i]); store8(tail + (pos - first) * LOCKS_D + hi, x[i] + 8); }
-        }
-      }
-    }
-    // ---- query rows of the page's new tokens, four of a thread's at a time
-    if (p.qo.p) {
-      constexpr int kAhead = 4;
-      const int rows = (t1 - t0) * p.Hq;
-      for (int r0 = tid >> 3; r0 < rows; r0 += kAhead * kQThreads / 8) {
-        Raw<__nv_bfloat16> y[kAhead];
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-          const int r = r0 + i * kQThreads / 8, t = r / p.Hq, h = r - t * p.Hq;
-          if (r < rows) y[i].load(reinterpret_cast<const __nv_bfloat16 *>(p.q.p) + (int64_t)(row0 + t0 + t - start) * p.q.st + (int64_t)h * p.q.sh, lo, hi);
-        }
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-          const int r = r0 + i * kQThreads / 8, t = r / p.Hq, h = r - t * p.Hq;
-          if (r >= rows) break;
-          if (mine) {
-            float x[16];
-            y[i].get(x);
-            turned(x, t);
-            y[i].set(x);
-          }
-          y[i].store(reinterpret_cast<__nv_bfloat16 *>(const_cast<char *>(p.qo.p)) + (int64_t)(row0 + t0 + t - start) * p.qo.st + (int64_t)h * p.qo.sh, lo, hi);
         }
       }
     }
@@ -482,11 +472,15 @@ int append_ok(const locks_ctx *c, const locks_rotary *rot, const int32_t *cu, in
 
 // Token rows a CTA: one while there are CTAs to spare, up to eight (a token's chain of lengths, block and angles is then paid once for
 // several)
+int rows_per_cta(const locks_ctx *c, int n) { return std::min((n - 1) / (4 * c->num_sms) + 1, kRopeTokens); }
 template <bool APPEND> void launch_rows(locks_ctx *c, RopeParams &p, cudaStream_t st) {
-  p.tokens = std::min(std::max(p.n / (4 * c->num_sms), 1), kRopeTokens);
-  const dim3 grid((p.n - 1) / p.tokens + 1);
-  if (c->cfg.kv_dtype == LOCKS_BF16) locks_launch_pdl(rope_rows_kernel<__nv_bfloat16, APPEND>, grid, dim3(kRopeThreads), 0, st, p);
-  else locks_launch_pdl(rope_rows_kernel<float, APPEND>, grid, dim3(kRopeThreads), 0, st, p);
+  p.tokens = rows_per_cta(c, p.n);
+  const dim3 grid((p.n - 1) / p.tokens + 1), block(kRopeThreads);
+  const bool bf = c->cfg.kv_dtype == LOCKS_BF16;
+  if (p.tokens == 1 && bf) locks_launch_pdl(rope_rows_kernel<__nv_bfloat16, APPEND, true>, grid, block, 0, st, p);
+  else if (p.tokens == 1) locks_launch_pdl(rope_rows_kernel<float, APPEND, true>, grid, block, 0, st, p);
+  else if (bf) locks_launch_pdl(rope_rows_kernel<__nv_bfloat16, APPEND, false>, grid, block, 0, st, p);
+  else locks_launch_pdl(rope_rows_kernel<float, APPEND, false>, grid, block, 0, st, p);
 }
 
 }  // namespace
@@ -538,16 +532,22 @@ extern "C" int locks_kvq_append(locks_ctx *ctx, const locks_rotary *rot, const i
   int rc = kvq_check(ctx, kv, batch);
   if (rc != LOCKS_OK) return rc;
   if ((rc = append_ok(ctx, rot, cu_tokens, num_tokens, q, q_out, k_new, v_new, batch)) != LOCKS_OK) return rc;
-  QAppendParams p = {};
+  QAppendParams a = {};
+  RopeParams &p = a.r;
   if (rot) p.rot = *rot;
   p.positions = positions; p.cu = cu_tokens; p.n = num_tokens; p.batch = batch;
   p.q = rows(q); p.qo = rows(q_out); p.k = rows(k_new); p.v = rows(v_new);
-  p.Hq = ctx->cfg.num_q_heads; p.c = kvq_cache(ctx, kv); p.status = ctx->status;
+  p.Hq = q ? ctx->cfg.num_q_heads : 0;
+  p.seq_lens = kv->seq_lens; p.B = ctx->B; p.Pmax = ctx->Pmax; p.status = ctx->status;
+  p.tokens = rows_per_cta(ctx, num_tokens);
+  a.q_ctas = q ? (num_tokens - 1) / p.tokens + 1 : 0;
+  a.c = kvq_cache(ctx, kv); a.status = ctx->status;
   // a request with m new tokens completes at most (m + B - 1) / B pages, and has an item at least
-  const int64_t grid = cu_tokens ? (int64_t)num_tokens / ctx->B + batch : batch;
+  const int64_t grid = (cu_tokens ? (int64_t)num_tokens / ctx->B + batch : batch) + a.q_ctas;
+  if (grid > INT32_MAX) return LOCKS_ERR_TOO_LARGE;
   const size_t smem = (size_t)ctx->B * 64 * sizeof(float2);
   ctx->last_launches = 0;
-  if (kv->fmt == LOCKS_KVQ_INT) locks_launch_pdl(kvq_append_kernel<LOCKS_KVQ_INT>, dim3((unsigned)grid), dim3(kQThreads), smem, (cudaStream_t)stream, p);
-  else locks_launch_pdl(kvq_append_kernel<LOCKS_KVQ_FLOAT>, dim3((unsigned)grid), dim3(kQThreads), smem, (cudaStream_t)stream, p);
+  if (kv->fmt == LOCKS_KVQ_INT) locks_launch_pdl(kvq_append_kernel<LOCKS_KVQ_INT>, dim3((unsigned)grid), dim3(kQThreads), smem, (cudaStream_t)stream, a);
+  else locks_launch_pdl(kvq_append_kernel<LOCKS_KVQ_FLOAT>, dim3((unsigned)grid), dim3(kQThreads), smem, (cudaStream_t)stream, a);
   return locks_check_launch(ctx);
 }
