@@ -113,13 +113,20 @@ struct RopeParams {
 // unit.  A thread fetches four units at a time, of four tokens (ONE: of four of its heads), while it turns the four before.  Bound by
 // the chain of a few round trips when there are few tokens (lengths and offsets; block; and rows, which are fetched meanwhile), by
 // memory when there are many.
-constexpr int kRopeThreads = 128, kRopeTokens = 8, kAhead = 4;
+constexpr int kRopeThreads = 128, kRopeTokens = 16, kAhead = 4;
+
+struct RowsShared {
+  float2 cs[kRopeTokens][64];
+  int64_t at[kRopeTokens];   // the token's row in the cache (elements), or -1
+  int owner[kRopeTokens], pos[kRopeTokens];
+};
 
 template <typename T, bool APPEND, bool ONE, int NT>
-__device__ __forceinline__ void rope_rows(const RopeParams &p, int cta) {
-  __shared__ __align__(16) float2 cs_s[kRopeTokens][64];
-  __shared__ int owner_s[kRopeTokens], pos_s[kRopeTokens];
-  __shared__ int64_t at_s[kRopeTokens];   // the token's row in the cache (elements), or -1
+__device__ __forceinline__ void rope_rows(const RopeParams &p, int cta, RowsShared &sm) {
+  auto &cs_s = sm.cs;
+  auto &at_s = sm.at;
+  auto &owner_s = sm.owner;
+  auto &pos_s = sm.pos;
   const int tid = threadIdx.x, row0 = cta * p.tokens, toks = ONE ? 1 : min(p.tokens, p.n - row0), half = p.rot.rot_dim / 2, u = tid & 7, inter = p.rot.interleaved;
   constexpr int kEach = NT / 64, kTurns = ONE ? 1 : (kRopeTokens + kEach - 1) / kEach;
   const int f = tid & 63, t0 = tid >> 6;   // this thread's frequency, for tokens t0, t0 + kEach, ..
@@ -130,10 +137,16 @@ __device__ __forceinline__ void rope_rows(const RopeParams &p, int cta) {
   unit_runs(u, p.rot.rot_dim, inter, lo, hi);
   const int heads = p.Hq + p.Hk + p.Hv, hi_off = hi - lo;
   const bool mine = u < p.rot.rot_dim / 16;
-  // units in batches of kAhead: ONE: heads (tid >> 3) + NT / 8 (k + i) of the token; else head (tid >> 3) + NT / 8 (k / kRopeTokens), tokens k % kRopeTokens + i
-  const int passes = (heads + NT / 8 - 1) / (NT / 8), end = ONE ? passes : passes * kRopeTokens;
-  auto head_of = [&](int k, int i) { return (tid >> 3) + NT / 8 * (ONE ? k + i : k / kRopeTokens); };
-  auto token_of = [&](int k, int i) { return ONE ? 0 : k % kRopeTokens + i; };
+  // Units in batches of kAhead: of head (tid >> 3) + NT / 8 pass, tokens t .. t + kAhead - 1; ONE: of the token's heads of kAhead passes
+  const int passes = (heads + NT / 8 - 1) / (NT / 8), slots = ONE ? kAhead : (toks + kAhead - 1) / kAhead * kAhead;
+  struct Batch {
+    int pass, t;
+    __device__ __forceinline__ void on(int slots) {
+      if (ONE || (t += kAhead) == slots) { t = 0; pass += ONE ? kAhead : 1; }
+    }
+  };
+  auto head_of = [&](const Batch &k, int i) { return (tid >> 3) + NT / 8 * (ONE ? k.pass + i : k.pass); };
+  auto token_of = [&](const Batch &k, int i) { return ONE ? 0 : k.t + i; };
   struct Line { const char *p; int64_t st; };   // a head's row of the CTA's first token (values are chosen: a reference chosen would be fetched lane by lane)
   auto source = [&](int h) {
     const bool q = h < p.Hq, k = !q && h < p.Hq + p.Hk;
@@ -141,12 +154,15 @@ __device__ __forceinline__ void rope_rows(const RopeParams &p, int cta) {
     return Line{(q ? p.q.p : (k ? p.k.p : p.v.p)) + (row0 * st + (h - (q ? 0 : (k ? p.Hq : p.Hq + p.Hk))) * sh + lo) * (int64_t)sizeof(T), st * (int64_t)sizeof(T)};
   };
   Raw<T> x[2][kAhead];
-  auto fetch = [&](Raw<T> (&y)[kAhead], int k) {
+  Batch from = {0, 0}, to = {0, 0};
+  auto fetch = [&](Raw<T> (&y)[kAhead]) {
+    const Batch k = from;
+    from.on(slots);
     Line l = source(head_of(k, 0));
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       if (ONE && i) l = source(head_of(k, i));
-      if (k < end && head_of(k, i) < heads && token_of(k, i) < toks) y[i].load(reinterpret_cast<const T *>(l.p + token_of(k, i) * l.st), 0, hi_off);
+      if (head_of(k, i) < heads && token_of(k, i) < toks) y[i].load(reinterpret_cast<const T *>(l.p + token_of(k, i) * l.st), 0, hi_off);
     }
   };
   int pos[kTurns];
@@ -174,7 +190,7 @@ __device__ __forceinline__ void rope_rows(const RopeParams &p, int cta) {
       }
     }
   }
-  fetch(x[0], 0);
+  fetch(x[0]);
   if (APPEND) {
     __syncthreads();
     if (tid < toks) {
@@ -199,7 +215,9 @@ __device__ __forceinline__ void rope_rows(const RopeParams &p, int cta) {
       if (t0 + kEach * i < toks) cs_s[t0 + kEach * i][turn_at(f)] = turn(pos[i], inv);
   }
   __syncthreads();
-  auto give = [&](Raw<T> (&y)[kAhead], int k) {
+  auto give = [&](Raw<T> (&y)[kAhead]) {
+    const Batch k = to;
+    to.on(slots);
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       const int h = head_of(k, i), t = token_of(k, i);
@@ -224,19 +242,22 @@ __device__ __forceinline__ void rope_rows(const RopeParams &p, int cta) {
     }
   };
 #pragma unroll 1
-  for (int k = 0; k < end; k += 2 * kAhead) {
-    fetch(x[1], k + kAhead);
-    give(x[0], k);
-    fetch(x[0], k + 2 * kAhead);
-    if (k + kAhead < end) give(x[1], k + kAhead);
+  while (true) {
+    if (from.pass < passes) fetch(x[1]);
+    give(x[0]);
+    if (to.pass >= passes) break;
+    if (from.pass < passes) fetch(x[0]);
+    give(x[1]);
+    if (to.pass >= passes) break;
   }
 }
 
 template <typename T, bool APPEND, bool ONE>
 __global__ void __launch_bounds__(kRopeThreads) rope_rows_kernel(const __grid_constant__ RopeParams p) {
+  __shared__ __align__(16) RowsShared sm;
   pdl_trigger();
   pdl_wait();
-  rope_rows<T, APPEND, ONE, kRopeThreads>(p, blockIdx.x);
+  rope_rows<T, APPEND, ONE, kRopeThreads>(p, blockIdx.x, sm);
 }
 
 // ------------------------------------------------------------------------------------------------ the 8-bit cache
@@ -250,6 +271,11 @@ struct QAppendParams {
 constexpr int kMostTokens = 1 << 30;   // places stay far from 32 bits' end
 constexpr int kQWarps = 8, kQThreads = kQWarps * 32;
 
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
 // x / scale, rounded to nearest: the product with the rounded reciprocal, and one correction by the remainder (Markstein 1990), which
 // a multiply-add gives exactly
 __device__ __forceinline__ float quotient(float x, float scale, float inv) {
@@ -280,18 +306,23 @@ template <int FMT> __device__ __forceinline__ uint32_t code4(const float *v, flo
 template <int FMT>
 __global__ void __launch_bounds__(kQThreads, 2) kvq_append_kernel(const __grid_constant__ QAppendParams a) {
   extern __shared__ __align__(16) float2 cs_s[];   // [B][64]
-  __shared__ int found_s[4];         // request, item of it, first row, new tokens
+  __shared__ int found_s[5];         // request, item of it, first row, new tokens, length
   __shared__ int warp_s[kQWarps];
   __shared__ uint32_t amax_s[kQWarps];
   pdl_trigger();
   pdl_wait();
   const RopeParams &p = a.r;
   if ((int)blockIdx.x < a.q_ctas) {
-    if (p.tokens == 1) rope_rows<__nv_bfloat16, true, true, kQThreads>(p, blockIdx.x);
-    else rope_rows<__nv_bfloat16, true, false, kQThreads>(p, blockIdx.x);
+    if (p.tokens == 1) rope_rows<__nv_bfloat16, true, true, kQThreads>(p, blockIdx.x, *reinterpret_cast<RowsShared *>(cs_s));
+    else rope_rows<__nv_bfloat16, true, false, kQThreads>(p, blockIdx.x, *reinterpret_cast<RowsShared *>(cs_s));
     return;
   }
   const KvqCache &c = a.c;
+  // this thread's frequency (fetched lane by lane, so once)
+  const int f = threadIdx.x & 63;
+  float inv_freq = 0.f;
+  int axis = 0;
+  if (f < p.rot.rot_dim / 2) { inv_freq = p.rot.inv_freq[f]; axis = p.rot.axis[f]; }
   const int cta = blockIdx.x - a.q_ctas, ctas = gridDim.x - a.q_ctas;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, B = c.B;
   const int half = p.rot.rot_dim / 2, u = lane & 7, inter = p.rot.interleaved;
@@ -305,11 +336,11 @@ __global__ void __launch_bounds__(kQThreads, 2) kvq_append_kernel(const __grid_c
     int before = 0;
     for (int b0 = 0; b0 < p.batch; b0 += kQThreads) {
       const int i = b0 + tid;
-      int items = 0, c0 = 0, m = 0;
+      int items = 0, c0 = 0, m = 0, T = 0;
       if (i < p.batch) {
         c0 = p.cu[i];
         m = p.cu[i + 1] - c0;
-        const int T = c.seq_lens[i];
+        T = c.seq_lens[i];
         if (m != 0 && (m < 0 || m > T || T > kMostTokens || c0 < 0 || c0 > p.n - m)) {
           set_status(a.status, LOCKS_ERR_BAD_BLOCK);
           m = 0;
@@ -331,7 +362,7 @@ __global__ void __launch_bounds__(kQThreads, 2) kvq_append_kernel(const __grid_c
         all += warp_s[w];
       }
       const int at = cta - before - (sum - items);
-      if (at >= 0 && at < items) { found_s[0] = i; found_s[1] = at; found_s[2] = c0; found_s[3] = m; }
+      if (at >= 0 && at < items) { found_s[0] = i; found_s[1] = at; found_s[2] = c0; found_s[3] = m; found_s[4] = T; }
       before += all;
       __syncthreads();
       if (before > cta && cta + 1 < ctas) break;   // (the last CTA looks at every request)
@@ -339,7 +370,7 @@ __global__ void __launch_bounds__(kQThreads, 2) kvq_append_kernel(const __grid_c
     if (found_s[0] < 0) return;
     b = found_s[0]; item = found_s[1]; row0 = found_s[2]; n = found_s[3];
   }
-  const int T = c.seq_lens[b], start = T - n;
+  const int T = p.cu ? found_s[4] : c.seq_lens[b], start = T - n;
   if (start < 0 || T > kMostTokens) {   // (one token per request: none at a length of zero)
     if (tid == 0 && T != 0) set_status(a.status, LOCKS_ERR_BAD_BLOCK);
     return;
@@ -348,10 +379,16 @@ __global__ void __launch_bounds__(kQThreads, 2) kvq_append_kernel(const __grid_c
   auto do_page = [&](int page) {
     const int first = page * B, t0 = max(first, start), t1 = min(first + B, T);
     const bool complete = first + B <= T;
-    for (int i = tid; i < (t1 - t0) * half; i += kQThreads) {
-      const int t = i / half, f = i - t * half, row = row0 + t0 + t - start;
-      cs_s[t * 64 + turn_at(f)] = turn(p.positions ? p.positions[(int64_t)p.rot.axis[f] * p.n + row] : t0 + t, p.rot.inv_freq[f]);
-    }
+    const int tasks = 2 * c.Hkv, per_round = kQWarps >> sub_shift, sub = warp & ((1 << sub_shift) - 1), at0 = first + 16 * sub + (lane >> 3);
+    auto row_at = [&](int task, int pos) {
+      const bool key = !(task & 1);
+      return reinterpret_cast<const __nv_bfloat16 *>(key ? p.k.p : p.v.p) + (int64_t)(row0 + pos - start) * (key ? p.k.st : p.v.st) + (int64_t)(task >> 1) * (key ? p.k.sh : p.v.sh);
+    };
+    if (f < half)
+      for (int t = t0 + (tid >> 6); t < t1; t += kQThreads / 64) {
+        const int row = row0 + t - start;
+        cs_s[(t - t0) * 64 + turn_at(f)] = turn(p.positions ? p.positions[(int64_t)axis * p.n + row] : t, inv_freq);
+      }
     int block = -1;
     if (complete) {
       if (page < c.Pmax) block = c.block_table[(int64_t)b * c.Pmax + page];
@@ -368,14 +405,13 @@ __global__ void __launch_bounds__(kQThreads, 2) kvq_append_kernel(const __grid_c
       unit_turn(x, cs, inter);
     };
     // ---- keys and values
-    const int tasks = 2 * c.Hkv, per_round = kQWarps >> sub_shift, sub = warp & ((1 << sub_shift) - 1), at0 = first + 16 * sub + (lane >> 3);
     __syncthreads();   // the cosines are there
     for (int r = 0; r < tasks; r += per_round) {
       const int task = r + (warp >> sub_shift), h = task >> 1;
       const bool live = task < tasks, key = !(task & 1);
       float *tail = (key ? c.kt : c.vt) + (((int64_t)b * c.Hkv + h) * B) * LOCKS_D;
       float x[4][16];
-      uint32_t amax = 0;
+      float top = 0.f;
       if (live) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -383,7 +419,7 @@ __global__ void __launch_bounds__(kQThreads, 2) kvq_append_kernel(const __grid_c
           if (pos < t0) {
             if (complete) { load8(tail + (pos - first) * LOCKS_D + lo, x[i]); load8(tail + (pos - first) * LOCKS_D + hi, x[i] + 8); }
           } else if (pos < t1) {
-            const __nv_bfloat16 *s = reinterpret_cast<const __nv_bfloat16 *>(key ? p.k.p : p.v.p) + (int64_t)(row0 + pos - start) * (key ? p.k.st : p.v.st) + (int64_t)h * (key ? p.k.sh : p.v.sh);
+            const __nv_bfloat16 *s = row_at(task, pos);
             load8(s + lo, x[i]);
             load8(s + hi, x[i] + 8);
           }
@@ -401,9 +437,9 @@ __global__ void __launch_bounds__(kQThreads, 2) kvq_append_kernel(const __grid_c
 #pragma unroll
           for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) amax = max(amax, __float_as_uint(x[i][e]) & 0x7fffffffu);   // (ordered as magnitudes, NaN last)
+            for (int e = 0; e < 16; ++e) top = max_nan(top, fabsf(x[i][e]));
         }
-        amax = __reduce_max_sync(0xffffffffu, amax);
+        uint32_t amax = __reduce_max_sync(0xffffffffu, __float_as_uint(top));   // (as whole numbers in the order of magnitudes, NaN last)
         if (sub_shift) {
           if (lane == 0) amax_s[warp] = amax;
           __syncthreads();
@@ -470,8 +506,8 @@ int append_ok(const locks_ctx *c, const locks_rotary *rot, const int32_t *cu, in
   return rot ? rotary_ok(rot) : LOCKS_OK;
 }
 
-// Token rows a CTA: one while there are CTAs to spare, up to eight (a token's chain of lengths, block and angles is then paid once for
-// several)
+// Token rows a CTA: one while there are CTAs to spare, then so many that all CTAs are there at once (a chain of lengths, blocks and
+// angles is paid once for all of a CTA's), up to sixteen
 int rows_per_cta(const locks_ctx *c, int n) { return std::min((n - 1) / (4 * c->num_sms) + 1, kRopeTokens); }
 template <bool APPEND> void launch_rows(locks_ctx *c, RopeParams &p, cudaStream_t st) {
   p.tokens = rows_per_cta(c, p.n);
@@ -545,7 +581,7 @@ extern "C" int locks_kvq_append(locks_ctx *ctx, const locks_rotary *rot, const i
   // a request with m new tokens completes at most (m + B - 1) / B pages, and has an item at least
   const int64_t grid = (cu_tokens ? (int64_t)num_tokens / ctx->B + batch : batch) + a.q_ctas;
   if (grid > INT32_MAX) return LOCKS_ERR_TOO_LARGE;
-  const size_t smem = (size_t)ctx->B * 64 * sizeof(float2);
+  const size_t smem = std::max((size_t)ctx->B * 64 * sizeof(float2), sizeof(RowsShared));
   ctx->last_launches = 0;
   if (kv->fmt == LOCKS_KVQ_INT) locks_launch_pdl(kvq_append_kernel<LOCKS_KVQ_INT>, dim3((unsigned)grid), dim3(kQThreads), smem, (cudaStream_t)stream, a);
   else locks_launch_pdl(kvq_append_kernel<LOCKS_KVQ_FLOAT>, dim3((unsigned)grid), dim3(kQThreads), smem, (cudaStream_t)stream, a);
