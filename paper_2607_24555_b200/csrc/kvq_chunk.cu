@@ -48,17 +48,45 @@ __device__ __forceinline__ float power_to(float amax, int top) {
 __device__ __forceinline__ void copy16(void *dst, const void *src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(smem_u32(dst)), "l"(src) : "memory");
 }
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];\n" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void ldsm4_trans(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];\n" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(*reinterpret_cast<unsigned long long *>(&d))
+      : "l"(*reinterpret_cast<unsigned long long *>(&a)), "l"(*reinterpret_cast<unsigned long long *>(&b)),
+        "l"(*reinterpret_cast<unsigned long long *>(&c)));
+  return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("mul.rn.f32x2 %0, %1, %2;"
+      : "=l"(*reinterpret_cast<unsigned long long *>(&d))
+      : "l"(*reinterpret_cast<unsigned long long *>(&a)), "l"(*reinterpret_cast<unsigned long long *>(&b)));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("add.rn.f32x2 %0, %1, %2;"
+      : "=l"(*reinterpret_cast<unsigned long long *>(&d))
+      : "l"(*reinterpret_cast<unsigned long long *>(&a)), "l"(*reinterpret_cast<unsigned long long *>(&b)));
+  return d;
+}
 // 16-byte piece `piece` of row `row` of an fp16 tile (rows of 256 bytes): pieces change places with the row, so that eight rows' pieces
 // of one ldmatrix lie in different banks
 __device__ __forceinline__ uint32_t at256(int row, int piece) { return row * 256 + ((piece ^ (row & 7)) << 4); }
 
 template <int FMT>
 __global__ void __launch_bounds__(kThreads, 2) kvq_chunk_kernel(const __grid_constant__ ChunkParams p) {
-  extern __shared__ __align__(128) uint8_t smem[];
+  extern __shared__ __align__(1024) uint8_t smem[];   // (rows of 256 bytes begin at multiples of 256: pieces change by exclusive or)
   float *scale_s = reinterpret_cast<float *>(smem + kOffMisc);       // [2 raw tiles][K, V][4 parts] and what is there: [2][4] ints behind
   int *kind_s = reinterpret_cast<int *>(smem + kOffMisc + 64);       // [2][4]: 0 nothing, 1 codes
   float *red_s = reinterpret_cast<float *>(smem + kOffMisc + 128);   // [2][kWarps]
-  __shared__ int found_s[4];
+  int *found_s = reinterpret_cast<int *>(smem + kOffMisc + 160);     // [4]
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, x = lane >> 2, t = lane & 3;
   const int Hkv = p.c.Hkv, h = blockIdx.x % Hkv, B = p.c.B;
   pdl_trigger();
@@ -200,50 +228,20 @@ __global__ void __launch_bounds__(kThreads, 2) kvq_chunk_kernel(const __grid_con
           for (int e = 0; e < 4; ++e) o[mt][nt][e] *= f;
     }
   };
-  // 32 tokens from row k0 of the K and V tiles on; their places start at pos.  ks, vs: of their two 16-token parts (vs relative to
-  // vref), ok0, ok1: whether they are there.  tail: the K tile's rows k0 + 32 .. hold what fp16 left of the keys in rows k0 ..; slow:
-  // values are taken from vt (fp32)
-  auto step = [&](int k0, int pos, float ks0, float ks1, float vs0, float vs1, bool ok0, bool ok1, bool tail, bool slow, const float *vt) {
-    float s[2][4][4];
+  // Scores (times f0, f1 for the two 16-token parts, in place) -> weights times the parts' value scales; a masked score is -inf already
+  auto weigh = [&](float (&s)[2][4][4], float ks0, float ks1, float vs0, float vs1, bool masked) {
 #pragma unroll
     for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-      for (int nt = 0; nt < 4; ++nt) s[mt][nt][0] = s[mt][nt][1] = s[mt][nt][2] = s[mt][nt][3] = 0.f;
-#pragma unroll 1
-    for (int part = 0; part < (tail ? 2 : 1); ++part) {
-      const int kr = k0 + 32 * part;
-#pragma unroll
-      for (int ks = 0; ks < 8; ++ks) {
-        uint32_t a[2][4], kf[2][4];
-#pragma unroll
-        for (int mt = 0; mt < 2; ++mt) ldsm_x4(a[mt], smem + at256(32 * warp + 16 * mt + (lane & 15), 2 * ks + (lane >> 4)));
-        // K rows are the columns of the second operand: matrices (tokens 0 .. 7, dims 0 .. 7), (0 .. 7, 8 .. 15), (8 .. 15, 0 .. 7), (8 .. 15, 8 .. 15)
-#pragma unroll
-        for (int g = 0; g < 2; ++g) ldsm_x4(kf[g], smem + kOffK + at256(kr + 16 * g + (lane & 7) + 8 * (lane >> 4), 2 * ks + ((lane >> 3) & 1)));
-#pragma unroll
-        for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-          for (int nt = 0; nt < 4; ++nt) mma_f16(s[mt][nt], a[mt][0], a[mt][1], a[mt][2], a[mt][3], kf[nt >> 1][2 * (nt & 1)], kf[nt >> 1][2 * (nt & 1) + 1]);
-      }
-    }
-    const bool mask = pos + 32 > seen0 || !(ok0 && ok1);   // some row does not see all of them
-    uint32_t pf[2][4][2];   // weights as A fragments: [rows][8 tokens][row x, x + 8]
-    float w[2][4][4];
-#pragma unroll
-    for (int mt = 0; mt < 2; ++mt) {
-#pragma unroll
       for (int c = 0; c < 2; ++c) {
         const float f0 = cr[mt][c] * ks0, f1 = cr[mt][c] * ks1;
-        float mx = -INFINITY;
+        float m0 = -INFINITY, m1 = -INFINITY;
 #pragma unroll
-        for (int nt = 0; nt < 4; ++nt)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            float &y = s[mt][nt][2 * c + e];
-            y *= nt < 2 ? f0 : f1;
-            if (mask && (pos + 8 * nt + 2 * t + e >= lim[mt][c] || !(nt < 2 ? ok0 : ok1))) y = -INFINITY;
-            mx = fmaxf(mx, y);
-          }
+        for (int nt = 0; nt < 2; ++nt) {
+          m0 = fmaxf(m0, fmaxf(s[mt][nt][2 * c], s[mt][nt][2 * c + 1]));
+          m1 = fmaxf(m1, fmaxf(s[mt][nt + 2][2 * c], s[mt][nt + 2][2 * c + 1]));
+        }
+        float mx = fmaxf(m0 * f0, m1 * f1);
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
         const float mn = fmaxf(m[mt][c], mx), ms = mn == -INFINITY ? 0.f : mn;
@@ -254,25 +252,82 @@ __global__ void __launch_bounds__(kThreads, 2) kvq_chunk_kernel(const __grid_con
           for (int nt = 0; nt < 16; ++nt) { o[mt][nt][2 * c] *= a; o[mt][nt][2 * c + 1] *= a; }
         }
         m[mt][c] = mn;
+        const float2 off = make_float2(15.f - ms, 15.f - ms);
+        float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int nt = 0; nt < 4; ++nt) {
+          const float f = nt < 2 ? f0 : f1, v = nt < 2 ? vs0 : vs1;
+          const float2 y = fma2(make_float2(s[mt][nt][2 * c], s[mt][nt][2 * c + 1]), make_float2(f, f), off);
+          const float2 q = make_float2(ex2f(y.x), ex2f(y.y));
+          sum = add2(sum, q);
+          float2 w = mul2(q, make_float2(v, v));
+          if (masked) {   // (nothing of a scale of NaN)
+            if (s[mt][nt][2 * c] == -INFINITY) w.x = 0.f;
+            if (s[mt][nt][2 * c + 1] == -INFINITY) w.y = 0.f;
+          }
+          s[mt][nt][2 * c] = w.x;
+          s[mt][nt][2 * c + 1] = w.y;
+        }
+        l[mt][c] += sum.x + sum.y;
+      }
+  };
+  // ldmatrix addresses of this lane for piece 0 of the first row: rows are 256 bytes apart, pieces change by exclusive or
+  const uint32_t q_addr = smem_u32(smem) + at256(32 * warp + (lane & 15), lane >> 4);
+  // K rows are the columns of the second operand: matrices (tokens 0 .. 7, dims 0 .. 7), (0 .. 7, 8 .. 15), (8 .. 15, 0 .. 7), (8 .. 15, 8 .. 15)
+  const uint32_t k_addr = smem_u32(smem) + kOffK + at256((lane & 7) + 8 * (lane >> 4), (lane >> 3) & 1);
+  // 16 tokens by 16 dims of V, transposed: matrices (tokens 0 .. 7, dims 0 .. 7), (8 .. 15, 0 .. 7), (0 .. 7, 8 .. 15), (8 .. 15, 8 .. 15)
+  const uint32_t v_addr = smem_u32(smem) + kOffV + at256(lane & 15, lane >> 4);
+  // 32 tokens from row k0 of the K and V tiles on; their places start at pos.  ks, vs: of their two 16-token parts (vs relative to
+  // vref), ok0, ok1: whether they are there.  tail: the K tile's rows k0 + 32 .. hold what fp16 left of the keys in rows k0 ..; slow:
+  // values are taken from vt (fp32)
+  auto step = [&](int k0, int pos, float ks0, float ks1, float vs0, float vs1, bool ok0, bool ok1, bool tail, bool slow, const float *vt) {
+    float s[2][4][4];
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+      for (int nt = 0; nt < 4; ++nt) s[mt][nt][0] = s[mt][nt][1] = s[mt][nt][2] = s[mt][nt][3] = 0.f;
+    uint32_t k_row = k_addr + k0 * 256;
+#pragma unroll 1
+    for (int part = 0; part < (tail ? 2 : 1); ++part, k_row += 32 * 256) {
+#pragma unroll
+      for (int ks = 0; ks < 8; ++ks) {
+        uint32_t a[2][4], kf[2][4];
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt) ldsm4(a[mt], (q_addr ^ (32 * ks)) + 4096 * mt);
+#pragma unroll
+        for (int g = 0; g < 2; ++g) ldsm4(kf[g], (k_row ^ (32 * ks)) + 4096 * g);
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+          for (int nt = 0; nt < 4; ++nt) mma_f16(s[mt][nt], a[mt][0], a[mt][1], a[mt][2], a[mt][3], kf[nt >> 1][2 * (nt & 1)], kf[nt >> 1][2 * (nt & 1) + 1]);
+      }
+    }
+    if (pos + 32 > seen0 || !(ok0 && ok1)) {   // some row does not see all of them
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
         for (int nt = 0; nt < 4; ++nt)
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const float y = s[mt][nt][2 * c + e], q = ex2f(y - ms + 15.f);
-            l[mt][c] += q;
-            w[mt][nt][2 * c + e] = mask && y == -INFINITY ? 0.f : q * (nt < 2 ? vs0 : vs1);   // (nothing of a scale of NaN)
+          for (int e = 0; e < 4; ++e) {
+            const bool sees = pos + 8 * nt + 2 * t + (e & 1) < lim[mt][e >> 1] && (nt < 2 ? ok0 : ok1);
+            s[mt][nt][e] = sees ? s[mt][nt][e] * (nt < 2 ? ks0 : ks1) : -INFINITY;
           }
-      }
-#pragma unroll
-      for (int nt = 0; nt < 4; ++nt) { pf[mt][nt][0] = pack_f16(w[mt][nt][0], w[mt][nt][1]); pf[mt][nt][1] = pack_f16(w[mt][nt][2], w[mt][nt][3]); }
+      weigh(s, 1.f, 1.f, vs0, vs1, true);
+    } else {
+      weigh(s, ks0, ks1, vs0, vs1, false);
     }
+    uint32_t pf[2][4][2];   // weights as A fragments: [rows][8 tokens][row x, x + 8]
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+      for (int nt = 0; nt < 4; ++nt) { pf[mt][nt][0] = pack_f16(s[mt][nt][0], s[mt][nt][1]); pf[mt][nt][1] = pack_f16(s[mt][nt][2], s[mt][nt][3]); }
     if (!slow) {
 #pragma unroll
       for (int g = 0; g < 2; ++g)
 #pragma unroll
-        for (int d = 0; d < 8; ++d) {   // 16 tokens by 16 dims: matrices (tokens 0 .. 7, dims 0 .. 7), (8 .. 15, 0 .. 7), (0 .. 7, 8 .. 15), (8 .. 15, 8 .. 15), transposed
+        for (int d = 0; d < 8; ++d) {
           uint32_t vf[4];
-          ldsm_x4_trans(vf, smem + kOffV + at256(k0 + 16 * g + (lane & 15), 2 * d + (lane >> 4)));
+          ldsm4_trans(vf, ((v_addr + k0 * 256) ^ (32 * d)) + 4096 * g);
 #pragma unroll
           for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
@@ -291,7 +346,7 @@ __global__ void __launch_bounds__(kThreads, 2) kvq_chunk_kernel(const __grid_con
             for (int nt = 0; nt < 4; ++nt)
 #pragma unroll
               for (int e = 0; e < 2; ++e)
-                if ((k >> 3) == nt && (k & 1) == e) mine = w[mt][nt][2 * c + e];
+                if ((k >> 3) == nt && (k & 1) == e) mine = s[mt][nt][2 * c + e];
             const float y = __shfl_sync(0xffffffffu, mine, (lane & ~3) + ((k & 7) >> 1));
             if (pos + k < lim[mt][c]) {
 #pragma unroll
