@@ -14,11 +14,11 @@
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int kWarps = 4, kThreads = 32 * kWarps, kRows = 32 * kWarps, kTok = 64;
+constexpr int kMt = 1, kWarps = 8, kThreads = 32 * kWarps, kRows = 16 * kMt * kWarps, kTok = 64;   // kMt: 16-row tiles of a warp
 // shared memory: queries [128][256 bytes]; K and V tiles in fp16 [64][256 bytes] each; two raw tiles (K, V: [64][128 bytes] each)
 constexpr int kQBytes = kRows * 256, kHalfTile = kTok * 256, kRawTile = 2 * kTok * 128;
 constexpr int kOffK = kQBytes, kOffV = kOffK + kHalfTile, kOffRaw = kOffV + kHalfTile, kOffMisc = kOffRaw + 2 * kRawTile;
-constexpr int kSmem = kOffMisc + 2 * 64 + 64;   // scales of two raw tiles' four 16-token parts (K, V), reductions
+constexpr int kSmem = kOffMisc + 256;   // scales of two raw tiles' four 16-token parts (K, V), reductions
 
 struct ChunkParams {
   const __nv_bfloat16 *q;
@@ -86,7 +86,7 @@ __global__ void __launch_bounds__(kThreads, 2) kvq_chunk_kernel(const __grid_con
   float *scale_s = reinterpret_cast<float *>(smem + kOffMisc);       // [2 raw tiles][K, V][4 parts] and what is there: [2][4] ints behind
   int *kind_s = reinterpret_cast<int *>(smem + kOffMisc + 64);       // [2][4]: 0 nothing, 1 codes
   float *red_s = reinterpret_cast<float *>(smem + kOffMisc + 128);   // [2][kWarps]
-  int *found_s = reinterpret_cast<int *>(smem + kOffMisc + 160);     // [4]
+  int *found_s = reinterpret_cast<int *>(smem + kOffMisc + 192);     // [4]
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, x = lane >> 2, t = lane & 3;
   const int Hkv = p.c.Hkv, h = blockIdx.x % Hkv, B = p.c.B;
   pdl_trigger();
@@ -132,70 +132,72 @@ __global__ void __launch_bounds__(kThreads, 2) kvq_chunk_kernel(const __grid_con
   const int codes_end = min(min(last, full_pages * B), p.c.Pmax * B);   // of them, those in codes
   const int tiles = last > 0 ? (codes_end + kTok - 1) / kTok : 0;
 
-  // ---- queries: a thread per row, fp16 times a power of two
+  // ---- queries: fp16 times a power of two, two threads a row (64 dims each)
   float c_row;   // what undoes it, times sm_scale log2 e
   {
-    const int j = tid / p.G, g = tid - j * p.G;
+    const int qr = tid >> 1, i0 = 8 * (tid & 1), j = qr / p.G, g = qr - j * p.G;
     const uint4 *src = reinterpret_cast<const uint4 *>(p.q + ((int64_t)(row0 + j) * p.Hq + h * p.G + g) * LOCKS_D);
     float amax = 0.f;
-    if (tid < rows) {
-#pragma unroll 4
-      for (int i = 0; i < 16; ++i) {
+    if (qr < rows) {
+#pragma unroll
+      for (int i = i0; i < i0 + 8; ++i) {
         const uint4 w = src[i];
         const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) amax = fmaxf(amax, fmaxf(finite_abs(__uint_as_float(u[e] << 16)), finite_abs(__uint_as_float(u[e] & 0xFFFF0000u))));
       }
     }
+    amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
     const float up = power_to(amax, 0);
     c_row = p.c2 / up;
-#pragma unroll 4
-    for (int i = 0; i < 16; ++i) {
+#pragma unroll
+    for (int i = i0; i < i0 + 8; ++i) {
       uint4 w = make_uint4(0, 0, 0, 0);
-      if (tid < rows) w = src[i];
+      if (qr < rows) w = src[i];
       uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
       for (int e = 0; e < 4; ++e) u[e] = pack_f16(__uint_as_float(u[e] << 16) * up, __uint_as_float(u[e] & 0xFFFF0000u) * up);
-      *reinterpret_cast<uint4 *>(smem + at256(tid, i)) = make_uint4(u[0], u[1], u[2], u[3]);
+      *reinterpret_cast<uint4 *>(smem + at256(qr, i)) = make_uint4(u[0], u[1], u[2], u[3]);
     }
   }
-  // rows of this lane: 32 warp + 16 mt + x + 8 c; lane r of a warp has row r's factor
-  float cr[2][2];
-  int lim[2][2];
+  // rows of this lane: 16 kMt warp + 16 mt + x + 8 c; lane 2 r of a warp has row r's factor
+  float cr[kMt][2];
+  int lim[kMt][2];
 #pragma unroll
-  for (int mt = 0; mt < 2; ++mt)
+  for (int mt = 0; mt < kMt; ++mt)
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       const int r = 16 * mt + x + 8 * c;
-      cr[mt][c] = __shfl_sync(0xffffffffu, c_row, r);
-      lim[mt][c] = 32 * warp + r < rows ? seen0 + (32 * warp + r) / p.G : last;
+      cr[mt][c] = __shfl_sync(0xffffffffu, c_row, 2 * r);
+      lim[mt][c] = 16 * kMt * warp + r < rows ? seen0 + (16 * kMt * warp + r) / p.G : last;
     }
 
   // ---- raw tiles: 16-byte copies, and the scales of the four 16-token parts; block ids are fetched a tile ahead of them
-  int blk[4];
+  int blk[2];
   auto blocks = [&](int tile) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int pos = tile * kTok + 16 * i;
+    for (int i = 0; i < 2; ++i) {
+      const int pos = tile * kTok + 16 * ((tid >> 7) + 2 * i);
       blk[i] = pos < codes_end ? p.c.block_table[(int64_t)b * p.c.Pmax + pos / B] : -1;
     }
   };
   auto issue = [&](int tile, int stage) {
     uint8_t *raw = smem + kOffRaw + stage * kRawTile;
     if (tile < tiles) {
-      // a thread's copies: piece tid & 7 of tokens (tid >> 3) + 16 i, i.e. of part i
+      // a thread's copies: piece tid & 7 of token (tid >> 3) % 16 of parts (tid >> 7) + 2 i
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int pos = tile * kTok + 16 * i, block = blk[i];
+      for (int k = 0; k < 2; ++k) {
+        const int i = (tid >> 7) + 2 * k, pos = tile * kTok + 16 * i, block = blk[k];
         const bool good = block >= 0 && block < p.c.num_blocks;
-        if (!good && pos < codes_end && tid == 0) set_status(p.status, LOCKS_ERR_BAD_BLOCK);
-        uint8_t *dk = raw + (16 * i + (tid >> 3)) * 128 + (tid & 7) * 16;
+        const int tok = (tid >> 3) & 15;
+        if (!good && pos < codes_end && (tid & 127) == 0) set_status(p.status, LOCKS_ERR_BAD_BLOCK);
+        uint8_t *dk = raw + (16 * i + tok) * 128 + (tid & 7) * 16;
         if (good) {
-          const int64_t off = (int64_t)block * p.c.sb + (int64_t)h * p.c.sh + (int64_t)(pos % B + (tid >> 3)) * p.c.st + (tid & 7) * 16;
+          const int64_t off = (int64_t)block * p.c.sb + (int64_t)h * p.c.sh + (int64_t)(pos % B + tok) * p.c.st + (tid & 7) * 16;
           copy16(dk, p.c.k + off);
           copy16(dk + kRawTile / 2, p.c.v + off);
         }
-        if (tid == i) {
+        if ((tid & 127) == 0) {
           kind_s[4 * stage + i] = good;
           scale_s[8 * stage + i] = good ? p.c.ks[(int64_t)block * Hkv + h] : 0.f;
           scale_s[8 * stage + 4 + i] = good ? p.c.vs[(int64_t)block * Hkv + h] : 0.f;
@@ -206,11 +208,11 @@ __global__ void __launch_bounds__(kThreads, 2) kvq_chunk_kernel(const __grid_con
     cp_async_commit();
   };
 
-  float o[2][16][4];   // rows as above (c0 c1: row x, c2 c3: row x + 8), dims 8 nt + 2 t, + 1
-  float m[2][2], l[2][2];
+  float o[kMt][16][4];   // rows as above (c0 c1: row x, c2 c3: row x + 8), dims 8 nt + 2 t, + 1
+  float m[kMt][2], l[kMt][2];
   float vref = 0x1p-126f;   // a power of two, at least the largest value scale so far
 #pragma unroll
-  for (int mt = 0; mt < 2; ++mt) {
+  for (int mt = 0; mt < kMt; ++mt) {
 #pragma unroll
     for (int nt = 0; nt < 16; ++nt) o[mt][nt][0] = o[mt][nt][1] = o[mt][nt][2] = o[mt][nt][3] = 0.f;
     m[mt][0] = m[mt][1] = -INFINITY;
@@ -221,7 +223,7 @@ __global__ void __launch_bounds__(kThreads, 2) kvq_chunk_kernel(const __grid_con
       const float to = __uint_as_float(min(((__float_as_uint(vs) >> 23) & 255u) + 1u, 254u) << 23), f = vref / to;
       vref = to;
 #pragma unroll
-      for (int mt = 0; mt < 2; ++mt)
+      for (int mt = 0; mt < kMt; ++mt)
 #pragma unroll
         for (int nt = 0; nt < 16; ++nt)
 #pragma unroll
@@ -229,9 +231,9 @@ __global__ void __launch_bounds__(kThreads, 2) kvq_chunk_kernel(const __grid_con
     }
   };
   // Scores (times f0, f1 for the two 16-token parts, in place) -> weights times the parts' value scales; a masked score is -inf already
-  auto weigh = [&](float (&s)[2][4][4], float ks0, float ks1, float vs0, float vs1, bool masked) {
+  auto weigh = [&](float (&s)[kMt][4][4], float ks0, float ks1, float vs0, float vs1, bool masked) {
 #pragma unroll
-    for (int mt = 0; mt < 2; ++mt)
+    for (int mt = 0; mt < kMt; ++mt)
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         const float f0 = cr[mt][c] * ks0, f1 = cr[mt][c] * ks1;
@@ -272,7 +274,7 @@ __global__ void __launch_bounds__(kThreads, 2) kvq_chunk_kernel(const __grid_con
       }
   };
   // ldmatrix addresses of this lane for piece 0 of the first row: rows are 256 bytes apart, pieces change by exclusive or
-  const uint32_t q_addr = smem_u32(smem) + at256(32 * warp + (lane & 15), lane >> 4);
+  const uint32_t q_addr = smem_u32(smem) + at256(16 * kMt * warp + (lane & 15), lane >> 4);
   // K rows are the columns of the second operand: matrices (tokens 0 .. 7, dims 0 .. 7), (0 .. 7, 8 .. 15), (8 .. 15, 0 .. 7), (8 .. 15, 8 .. 15)
   const uint32_t k_addr = smem_u32(smem) + kOffK + at256((lane & 7) + 8 * (lane >> 4), (lane >> 3) & 1);
   // 16 tokens by 16 dims of V, transposed: matrices (tokens 0 .. 7, dims 0 .. 7), (8 .. 15, 0 .. 7), (0 .. 7, 8 .. 15), (8 .. 15, 8 .. 15)
@@ -281,9 +283,9 @@ __global__ void __launch_bounds__(kThreads, 2) kvq_chunk_kernel(const __grid_con
   // vref), ok0, ok1: whether they are there.  tail: the K tile's rows k0 + 32 .. hold what fp16 left of the keys in rows k0 ..; slow:
   // values are taken from vt (fp32)
   auto step = [&](int k0, int pos, float ks0, float ks1, float vs0, float vs1, bool ok0, bool ok1, bool tail, bool slow, const float *vt) {
-    float s[2][4][4];
+    float s[kMt][4][4];
 #pragma unroll
-    for (int mt = 0; mt < 2; ++mt)
+    for (int mt = 0; mt < kMt; ++mt)
 #pragma unroll
       for (int nt = 0; nt < 4; ++nt) s[mt][nt][0] = s[mt][nt][1] = s[mt][nt][2] = s[mt][nt][3] = 0.f;
     uint32_t k_row = k_addr + k0 * 256;
@@ -291,20 +293,20 @@ __global__ void __launch_bounds__(kThreads, 2) kvq_chunk_kernel(const __grid_con
     for (int part = 0; part < (tail ? 2 : 1); ++part, k_row += 32 * 256) {
 #pragma unroll
       for (int ks = 0; ks < 8; ++ks) {
-        uint32_t a[2][4], kf[2][4];
+        uint32_t a[kMt][4], kf[2][4];
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt) ldsm4(a[mt], (q_addr ^ (32 * ks)) + 4096 * mt);
+        for (int mt = 0; mt < kMt; ++mt) ldsm4(a[mt], (q_addr ^ (32 * ks)) + 4096 * mt);
 #pragma unroll
         for (int g = 0; g < 2; ++g) ldsm4(kf[g], (k_row ^ (32 * ks)) + 4096 * g);
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt)
+        for (int mt = 0; mt < kMt; ++mt)
 #pragma unroll
           for (int nt = 0; nt < 4; ++nt) mma_f16(s[mt][nt], a[mt][0], a[mt][1], a[mt][2], a[mt][3], kf[nt >> 1][2 * (nt & 1)], kf[nt >> 1][2 * (nt & 1) + 1]);
       }
     }
     if (pos + 32 > seen0 || !(ok0 && ok1)) {   // some row does not see all of them
 #pragma unroll
-      for (int mt = 0; mt < 2; ++mt)
+      for (int mt = 0; mt < kMt; ++mt)
 #pragma unroll
         for (int nt = 0; nt < 4; ++nt)
 #pragma unroll
@@ -316,9 +318,9 @@ __global__ void __launch_bounds__(kThreads, 2) kvq_chunk_kernel(const __grid_con
     } else {
       weigh(s, ks0, ks1, vs0, vs1, false);
     }
-    uint32_t pf[2][4][2];   // weights as A fragments: [rows][8 tokens][row x, x + 8]
+    uint32_t pf[kMt][4][2];   // weights as A fragments: [rows][8 tokens][row x, x + 8]
 #pragma unroll
-    for (int mt = 0; mt < 2; ++mt)
+    for (int mt = 0; mt < kMt; ++mt)
 #pragma unroll
       for (int nt = 0; nt < 4; ++nt) { pf[mt][nt][0] = pack_f16(s[mt][nt][0], s[mt][nt][1]); pf[mt][nt][1] = pack_f16(s[mt][nt][2], s[mt][nt][3]); }
     if (!slow) {
@@ -329,7 +331,7 @@ __global__ void __launch_bounds__(kThreads, 2) kvq_chunk_kernel(const __grid_con
           uint32_t vf[4];
           ldsm4_trans(vf, ((v_addr + k0 * 256) ^ (32 * d)) + 4096 * g);
 #pragma unroll
-          for (int mt = 0; mt < 2; ++mt)
+          for (int mt = 0; mt < kMt; ++mt)
 #pragma unroll
             for (int e = 0; e < 2; ++e)
               mma_f16(o[mt][2 * d + e], pf[mt][2 * g][0], pf[mt][2 * g][1], pf[mt][2 * g + 1][0], pf[mt][2 * g + 1][1], vf[2 * e], vf[2 * e + 1]);
@@ -338,7 +340,7 @@ __global__ void __launch_bounds__(kThreads, 2) kvq_chunk_kernel(const __grid_con
 #pragma unroll 1
       for (int k = 0; k < 32 && pos + k < T; ++k) {
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt)
+        for (int mt = 0; mt < kMt; ++mt)
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
             float mine = 0.f;
@@ -380,11 +382,11 @@ __global__ void __launch_bounds__(kThreads, 2) kvq_chunk_kernel(const __grid_con
       __syncthreads();   // the tile's bytes and scales are there; the last tile's fp16 form is used
       const uint8_t *raw = smem + kOffRaw + stage * kRawTile;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {   // 16 codes: piece tid & 7 of row (tid >> 3) + 16 i, of K for i < 4, then of V
-        const int row = (tid >> 3) + 16 * (i & 3), piece = tid & 7;
-        const bool key = i < 4;
+      for (int i = 0; i < 4; ++i) {   // 16 codes: piece tid & 7 of row (tid >> 3) + 32 (i % 2), of K for i < 2, then of V
+        const int row = (tid >> 3) + 32 * (i & 1), piece = tid & 7;
+        const bool key = i < 2;
         uint4 y = *reinterpret_cast<const uint4 *>(raw + (key ? 0 : kRawTile / 2) + row * 128 + piece * 16);
-        if (!kind_s[4 * stage + (i & 3)]) y = make_uint4(0, 0, 0, 0);
+        if (!kind_s[4 * stage + (row >> 4)]) y = make_uint4(0, 0, 0, 0);
         const uint32_t word[4] = {y.x, y.y, y.z, y.w};
         uint32_t f[8];
 #pragma unroll
@@ -398,9 +400,9 @@ __global__ void __launch_bounds__(kThreads, 2) kvq_chunk_kernel(const __grid_con
       kind = *reinterpret_cast<const int4 *>(kind_s + 4 * stage);
       __syncthreads();
     } else {
-      // a thread: 32 dims of one token, as fp16 times a power of two of the 32 tokens' largest; keys in two parts (22 bits)
+      // a thread: 16 dims of one token, as fp16 times a power of two of the 32 tokens' largest; keys in two parts (22 bits)
       pos = full_pages * B + 32 * (tile - tiles);
-      const int tok = tid >> 2, d0 = 32 * (tid & 3);
+      const int tok = tid >> 3, d0 = 16 * (tid & 7);
       const int64_t at = (((int64_t)b * Hkv + h) * B + pos - full_pages * B) * LOCKS_D;
       vt = p.c.vt + at;
       const float *src[2] = {p.c.kt + at + tok * LOCKS_D + d0, vt + tok * LOCKS_D + d0};
@@ -410,7 +412,7 @@ __global__ void __launch_bounds__(kThreads, 2) kvq_chunk_kernel(const __grid_con
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv)
 #pragma unroll 4
-          for (int i = 0; i < 32; ++i) {
+          for (int i = 0; i < 16; ++i) {
             const float y = src[kv][i];
             amax[kv] = fmaxf(amax[kv], finite_abs(y));
             if (kv == 1) odd |= !(fabsf(y) < INFINITY);
@@ -420,13 +422,18 @@ __global__ void __launch_bounds__(kThreads, 2) kvq_chunk_kernel(const __grid_con
 #pragma unroll
       for (int kv = 0; kv < 2; ++kv) {
         const float y = warp_max(amax[kv]);
-        if (lane == 0) red_s[4 * kv + warp] = y;
+        if (lane == 0) red_s[kWarps * kv + warp] = y;
       }
       slow = __syncthreads_or(odd);
 #pragma unroll
-      for (int kv = 0; kv < 2; ++kv) up[kv] = power_to(fmaxf(fmaxf(red_s[4 * kv], red_s[4 * kv + 1]), fmaxf(red_s[4 * kv + 2], red_s[4 * kv + 3])), 14);
+      for (int kv = 0; kv < 2; ++kv) {
+        float y = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) y = fmaxf(y, red_s[kWarps * kv + w]);
+        up[kv] = power_to(y, 14);
+      }
 #pragma unroll 1
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < 2; ++i) {
         uint32_t k_hi[4], k_lo[4], v_hi[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -461,13 +468,13 @@ __global__ void __launch_bounds__(kThreads, 2) kvq_chunk_kernel(const __grid_con
   cp_async_wait<0>();
   // ---- results
 #pragma unroll
-  for (int mt = 0; mt < 2; ++mt)
+  for (int mt = 0; mt < kMt; ++mt)
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       float sum = l[mt][c];
       sum += __shfl_xor_sync(0xffffffffu, sum, 1);
       sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-      const int r = 32 * warp + 16 * mt + x + 8 * c;
+      const int r = 16 * kMt * warp + 16 * mt + x + 8 * c;
       if (r >= rows) continue;
       const int j = r / p.G, g = r - j * p.G;
       const int64_t row = (int64_t)(row0 + j) * p.Hq + h * p.G + g;
