@@ -1,11 +1,14 @@
 // What the calls around a decode step share: rows, rotary positions, the 8-bit cache and their checks.
 #pragma once
+#include <algorithm>
 #include <cmath>
 
 #include "locks_internal.cuh"
 
 #define KVQ_SLOT_BOUND 592       // upper bound on the CTAs of the token attention kernel (148 SMs x 4)
 #define KVQ_ROWS 16              // query rows of a problem at most
+#define KVQ_CHUNK_SLOTS 148      // CTAs of the chunk attention kernel at most where it splits the tokens
+#define KVQ_CHUNK_ROWS 256       // query rows of one of them
 #define KVQ_TINY_BITS 0x0D800000u   // 2^-100: a page whose largest magnitude is below it is stored as zeros
 
 struct KvqCache {   // the 8-bit cache as the kernels take it
@@ -39,7 +42,9 @@ static inline int kvq_check(const locks_ctx *c, const locks_kvq *kv, int batch) 
 int locks_launch_kvq_chunk(locks_ctx *c, const void *q, const int32_t *cu, int n, const locks_kvq *kv, int batch, void *out, float *lse, cudaStream_t st);
 
 // token attention: partials of the problems that several CTAs share, of whom each leaves at most two
-static inline size_t kvq_part_floats() { return (size_t)2 * KVQ_SLOT_BOUND * KVQ_ROWS * LOCKS_D; }
+// chunk attention: of 256 rows in each CTA of its splits, with one number a row
+static_assert(KVQ_CHUNK_SLOTS * KVQ_CHUNK_ROWS <= 4 * KVQ_SLOT_BOUND * KVQ_ROWS, "");
+static inline size_t kvq_part_floats() { return (size_t)std::max(2 * KVQ_SLOT_BOUND * KVQ_ROWS, KVQ_CHUNK_SLOTS * KVQ_CHUNK_ROWS) * LOCKS_D; }
 static inline size_t kvq_ml_floats() { return (size_t)2 * KVQ_SLOT_BOUND * KVQ_ROWS * 2; }
 
 #ifdef __CUDACC__

@@ -877,10 +877,13 @@ extern "C" int locks_kvq_attend(locks_ctx *ctx, const void *q, const int32_t *cu
   if (ctx->cfg.combine == LOCKS_COMBINE_PER_HEAD && page_ids) { p.kvdiv = p.G; p.Hkv = p.Hq; p.G = 1; }   // a page table per query head
   p.sub_shift = ctx->B == 64 ? 2 : (ctx->B == 32 ? 1 : 0);
   p.c2 = ctx->cfg.sm_scale * kLog2e;
-  // Chunks of prompts: 128 rows a tile, where that gives every SM a tile, or where the line of the other form may not fit 32 bits
+  // Chunks of prompts, from 96 query rows a KV head and request on average, and 768 in all (20 to 24 tokens of 32 heads): the form with 256
+  // rows a CTA.  Measured either side, us, this form and that, 32 query heads: one request at 16301 with 8 KV heads 41 / 43 (16 tokens),
+  // 58 / 47 (32), 183 / 73 (128), 1361 / 362 (1024); six at 6000 113 / 58 (32 each); with 2 KV heads 38 / 32 (8 each); 24 at 3000 with 8 KV
+  // heads 132 / 138 (16 each), 246 / 138 (32).  Also where the line of this form may not fit 32 bits.
   const int64_t problem = (((int64_t)(page_ids ? p.kbud : p.c.Pmax) << p.sub_shift) + 1) / 2 + kMostLead;   // places at most
   const bool fits = (batch + (cu_tokens ? (int64_t)num_tokens : 0)) * p.Hkv * problem <= INT32_MAX;
-  if (cu_tokens && (!fits || (int64_t)num_tokens * p.G / 128 * p.Hkv >= ctx->num_sms)) {
+  if (cu_tokens && (!fits || ((int64_t)num_tokens * p.G >= (int64_t)96 * batch && (int64_t)num_tokens * p.Hq >= 768))) {
     ctx->last_launches = 0;
     return locks_launch_kvq_chunk(ctx, q, cu_tokens, num_tokens, kv, batch, out, lse, (cudaStream_t)stream);
   }

@@ -13,7 +13,16 @@
 // the largest value scale so far.  A row's weights are 2^8 p relative to a maximum that may be exceeded by 2^8 before the output is
 // rescaled (in tensor memory: rarely more than once or twice a row), so they stay below 2^15, and normal in fp16 down to 2^-20 of the
 // largest.
-// BOUNDS
+//
+// Why 2 x 128 rows: a tile's conversion and its way through shared memory serve twice as many rows, and the two take turns on the tensor
+// cores.  Why the scores are read once: a maximum that may be exceeded needs no second pass, and the next 32 columns' maximum hides
+// between these 32's exponentials.  Registers are split by warps' kind (setmaxnreg).  Where blocks of 256 rows are fewer than SMs, the
+// tokens that each sees are shared by several CTAs, and a second kernel joins them.
+// Measured, 1024 tokens of 32 heads over 8 KV heads after 15277: 362 us, 701 TFLOP/s, 0.44 of a library matrix product's rate (with 128 of 148
+// SMs at work: a CTA for each block); without the softmax 252, without products and conversion 276.  Pipes are about half busy
+// (exponentials 50 %, tensor cores 40 %, issue 43 %): bound by the latencies of a chain of softmax and products with two softmax warps a
+// scheduler.  One request's tokens after 16K: 47 us (32 tokens), 73 (128), 205 (512).  Accumulators add up in the tensor cores' fp32.
+#include <algorithm>
 #include <type_traits>
 
 #include "kvq.cuh"
@@ -35,7 +44,7 @@ struct Misc {
   float scale[2][2][kParts];   // [stage][K, V][16-token part]
   uint32_t there[2];           // [stage]: a bit per part
   float red[16];
-  int found[4];
+  int found[6];
   uint32_t tmem;
   int slow;                    // the unfinished page has values that are not finite
 };
@@ -50,9 +59,9 @@ struct ChunkParams {
   const int32_t *cu;
   KvqCache c;
   __nv_bfloat16 *out;
-  float *lse;
+  float *lse, *part, *part_lse;   // (partials of the splits: [block, head][split][2 x 128 rows], normalised, and log2 of their sums)
   int32_t *status;
-  int n, batch, Hq, G, tile_tokens, log_b;   // tile_tokens: of 128 rows
+  int n, batch, Hq, G, tile_tokens, log_b, slots;   // slots: CTAs that may leave partials   // tile_tokens: of 128 rows
   float c2;
 };
 
@@ -143,49 +152,69 @@ __device__ __forceinline__ constexpr uint32_t instruction() { return 1u << 4 | (
 
 __device__ __forceinline__ uint32_t f32_bits(float x) { return __float_as_uint(x); }
 
-template <int FMT>
-__global__ void __launch_bounds__(kThreads, 1) kvq_chunk_kernel(const __grid_constant__ ChunkParams p) {
-  extern __shared__ __align__(1024) uint8_t smem[];
-  Misc &ms = *reinterpret_cast<Misc *>(smem + kOffMisc);
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int Hkv = p.c.Hkv, h = blockIdx.x % Hkv, B = p.c.B, cta_tokens = 2 * p.tile_tokens;
-  pdl_trigger();
-  pdl_wait();
-  // ---- the rows of this CTA: a request's from the last ones on, so that the ones that see most start first
-  if (tid == 0) {
-    ms.found[0] = -1;
-    ms.slow = 0;
-  }
+// A unit of work: a block of 2 tile_tokens tokens of a request, and which share of the tokens that it sees.  Blocks are numbered request
+// by request, a request's from the last one on, so that the ones that see most start first; where there are few, each is split so that
+// the slots are all used.
+struct Block {
+  int b, j0, row0, n;   // request (< 0: none), its token and row at which the block starts, tokens of the request
+  int index, splits;
+};
+// unit: index * per_index * splits + something smaller, or the index itself (per_index 0)
+__device__ __forceinline__ Block find_block(const ChunkParams &p, int unit, int per_index, int (&found)[6]) {
+  const int tokens = 2 * p.tile_tokens;
+  if (threadIdx.x == 0) found[0] = -1;
   __syncthreads();
-  if (warp == 0) {
-    int before = 0;
-    const int want = blockIdx.x / Hkv;
-    for (int b0 = 0; b0 < p.batch; b0 += 32) {
-      int n = 0, row0 = 0;
-      if (b0 + lane < p.batch) {
-        row0 = p.cu[b0 + lane];
-        n = p.cu[b0 + lane + 1] - row0;
+  if (threadIdx.x < 32) {
+    const int lane = threadIdx.x;
+    auto blocks_of = [&](int b, int &row0, int &n) -> int {
+      n = row0 = 0;
+      if (b < p.batch) {
+        row0 = p.cu[b];
+        n = p.cu[b + 1] - row0;
         if (n < 0 || row0 < 0 || row0 > p.n - n) {
           set_status(p.status, LOCKS_ERR_BAD_BLOCK);
           n = 0;
         }
       }
-      const int tiles = (n + cta_tokens - 1) / cta_tokens;
-      int end = tiles;
+      return (n + tokens - 1) / tokens;
+    };
+    int total = 0, row0, n;
+    for (int b0 = 0; b0 < p.batch; b0 += 32) total += blocks_of(b0 + lane, row0, n);
+    total = __reduce_add_sync(0xffffffffu, total);
+    const int splits = max(1, p.slots / max(1, min(total, p.slots) * p.c.Hkv)), want = per_index ? unit / (per_index * splits) : unit;
+    int before = 0;
+    for (int b0 = 0; b0 < p.batch && before <= want; b0 += 32) {
+      const int blocks = blocks_of(b0 + lane, row0, n);
+      int end = blocks;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const int y = __shfl_up_sync(0xffffffffu, end, o);
         if (lane >= o) end += y;
       }
-      const int at = want - before - (end - tiles);
-      if (at >= 0 && at < tiles) { ms.found[0] = b0 + lane; ms.found[1] = tiles - 1 - at; ms.found[2] = row0; ms.found[3] = n; }
+      const int at = want - before - (end - blocks);
+      if (at >= 0 && at < blocks) { found[0] = b0 + lane; found[1] = blocks - 1 - at; found[2] = row0; found[3] = n; }
       before += __shfl_sync(0xffffffffu, end, 31);
     }
+    if (lane == 0) { found[4] = want; found[5] = splits; }
   }
   __syncthreads();
-  const int b = ms.found[0];
+  const int j0 = found[1] * tokens;
+  return Block{found[0], j0, found[2] + j0, found[3], found[4], found[5]};
+}
+
+template <int FMT>
+__global__ void __launch_bounds__(kThreads, 1) kvq_chunk_kernel(const __grid_constant__ ChunkParams p) {
+  extern __shared__ __align__(1024) uint8_t smem[];
+  Misc &ms = *reinterpret_cast<Misc *>(smem + kOffMisc);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int Hkv = p.c.Hkv, B = p.c.B, cta_tokens = 2 * p.tile_tokens;
+  pdl_trigger();
+  pdl_wait();
+  if (tid == 0) ms.slow = 0;
+  const Block at = find_block(p, blockIdx.x, Hkv, ms.found);
+  const int b = at.b, j0 = at.j0, row0 = at.row0, n = at.n;
   if (b < 0) return;
-  const int j0 = ms.found[1] * cta_tokens, row0 = ms.found[2] + j0, n = ms.found[3];
+  const int splits = at.splits, split = blockIdx.x % splits, h = blockIdx.x / splits % Hkv;
   const int toks = min(cta_tokens, n - j0), halves = toks > p.tile_tokens ? 2 : 1;   // of 128 rows
   const int T = max(p.c.seq_lens[b], 0);
   const int seen0 = T - n + j0 + 1;      // tokens that the CTA's first token sees
@@ -193,9 +222,11 @@ __global__ void __launch_bounds__(kThreads, 1) kvq_chunk_kernel(const __grid_con
   if (T > 0 && (T - 1) >> p.log_b >= p.c.Pmax && tid == 0) set_status(p.status, LOCKS_ERR_BAD_BLOCK);
   const int last = min(min(seen0 + toks - 1, T), p.c.Pmax * B);   // tokens that the CTA's last token sees
   const int codes_end = min(last, full_pages * B);                // of them, those in codes
-  const int tiles = last > 0 ? (codes_end + kTok - 1) / kTok : 0;
-  const int tail_tiles = full_pages < p.c.Pmax && last > full_pages * B;   // the unfinished page: fewer than 64 tokens
-  const int nt = tiles + tail_tiles;
+  // ---- tiles of 128 tokens, then the unfinished page (fewer than 64); of them this CTA's share: nt from tile0 on, `tiles` of them codes
+  const int all_codes = last > 0 ? (codes_end + kTok - 1) / kTok : 0;
+  const int64_t all = all_codes + (full_pages < p.c.Pmax && last > full_pages * B);
+  const int tile0 = (int)(all * split / splits), nt = (int)(all * (split + 1) / splits) - tile0;
+  const int tiles = min(max(all_codes - tile0, 0), nt), tail_tiles = nt - tiles;
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(&ms.kv_full[i], kConv); mbar_init(&ms.kv_empty[i], 1);
@@ -262,16 +293,17 @@ __global__ void __launch_bounds__(kThreads, 1) kvq_chunk_kernel(const __grid_con
     int blk[4], my_blk = 0, my_there = 0;   // (my_blk: of part ct % 8, whose scale of K, V threads 0 .. 7, 8 .. 15 fetch)
     uint4 k[4], v[4];
     float my_scale = 0.f;
-    const int32_t *row = p.c.block_table + (int64_t)b * p.c.Pmax;
+    const int left = codes_end - tile0 * kTok;   // tokens in codes from tile0 on, and their pages
+    const int32_t *row = p.c.block_table + (int64_t)b * p.c.Pmax + ((tile0 * kTok) >> p.log_b);
     const char *kp = p.c.k + (int64_t)h * p.c.sh + piece * 16, *vp = p.c.v + (int64_t)h * p.c.sh + piece * 16;
     auto blocks = [&](int tile) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int pos = tile * kTok + 32 * i + (tok & 16);
-        blk[i] = pos < codes_end ? row[pos >> p.log_b] : -1;
+        blk[i] = pos < left ? row[pos >> p.log_b] : -1;
       }
       const int pos = tile * kTok + 16 * (ct & 7);
-      my_blk = pos < codes_end ? row[pos >> p.log_b] : -1;
+      my_blk = pos < left ? row[pos >> p.log_b] : -1;
     };
     auto is_there = [&](int block) { return (uint32_t)block < (uint32_t)p.c.num_blocks; };
     auto fetch = [&](int tile) {
@@ -284,7 +316,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvq_chunk_kernel(const __grid_con
         v[i] = load_if(vp + off, good);
       }
       my_there = is_there(my_blk);
-      if (!my_there && tile * kTok + 16 * (ct & 7) < codes_end) set_status(p.status, LOCKS_ERR_BAD_BLOCK);
+      if (!my_there && tile * kTok + 16 * (ct & 7) < left) set_status(p.status, LOCKS_ERR_BAD_BLOCK);
       my_scale = ct < 16 && my_there ? (ct < 8 ? p.c.ks : p.c.vs)[(int64_t)my_blk * Hkv + h] : 0.f;
       blocks(tile + 1);
     };
@@ -386,12 +418,21 @@ __global__ void __launch_bounds__(kThreads, 1) kvq_chunk_kernel(const __grid_con
   } else {
     // ------------------------------------------------------------------------------------------ softmax: thread = row
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(kSoftRegs));
-    const int t = warp >> 2, r = tid & 127, jr = t * p.tile_tokens + r / p.G, g = r % p.G;
-    const bool real = r < p.tile_tokens * p.G && jr < toks;
-    const int first = seen0 + t * p.tile_tokens;   // tokens that the first of these 128 rows sees
-    const int64_t row = (int64_t)(row0 + jr) * p.Hq + h * p.G + g;
+    const int t = warp >> 2, r = tid & 127;
+    const int first = seen0 + t * p.tile_tokens - tile0 * kTok;   // tokens from tile0 on that the first of these 128 rows sees
+    // this thread's token within the CTA, and its row of q and out (asked for again after the loop, so that the loop need not keep them)
+    auto place = [&](int r, int &jr, int64_t &row) -> bool {
+      jr = t * p.tile_tokens + r / p.G;
+      row = (int64_t)(row0 + jr) * p.Hq + h * p.G + r % p.G;
+      return r < p.tile_tokens * p.G && jr < toks;
+    };
     float cr;
+    int lim;   // this row sees the first lim tokens from tile0 on
     {
+      int jr;
+      int64_t row;
+      const bool real = place(r, jr, row);
+      lim = (real ? seen0 + jr : last) - tile0 * kTok;
       const uint4 *src = reinterpret_cast<const uint4 *>(p.q + row * LOCKS_D);
       float amax = 0.f;
       if (real) {
@@ -417,7 +458,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvq_chunk_kernel(const __grid_con
     }
     fence_async_proxy();
     mbar_arrive(&ms.q_full);
-    const int lim = real ? seen0 + jr : last;   // this row sees the first lim tokens
+    const int tail_pos = full_pages * B - tile0 * kTok;
     const uint32_t s_at = tmem + 128 * t + ((uint32_t)(32 * (warp & 3)) << 16), o_at = s_at + kColO;
     float m = -INFINITY, l = 0.f;                  // m: a whole number
     float vref = 0x1p-126f, inv = 0x1p126f;   // values' reference, 1 / vref
@@ -425,7 +466,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvq_chunk_kernel(const __grid_con
     for (int j = 0; j < mine && ok; ++j) {
       const int stage = j & 1;
       const bool tail = j >= tiles;
-      const int pos = tail ? full_pages * B : j * kTok;
+      const int pos = tail ? tail_pos : j * kTok;
       ok = mbar_wait(&ms.s_full[t], j & 1) && mbar_wait(&ms.kv_full[stage], (j >> 1) & 1);   // (the second: the scales)
       if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
       fence_after();
@@ -569,6 +610,10 @@ __global__ void __launch_bounds__(kThreads, 1) kvq_chunk_kernel(const __grid_con
     if (mine > 0 && ok) ok = mbar_wait(&ms.o_full, 0);
     const bool good = __all_sync(0xffffffffu, ok);
     fence_after();
+    int jr, again = r;
+    int64_t row;
+    asm volatile("" : "+r"(again));
+    const bool real = place(again, jr, row);
     const float scale = l == 0.f ? 0.f : vref / l;   // (0: nothing seen)
     const bool slow = tail_tiles > 0 && ms.slow;     // (written before the last tile's barrier)
 #pragma unroll 1
@@ -584,14 +629,19 @@ __global__ void __launch_bounds__(kThreads, 1) kvq_chunk_kernel(const __grid_con
       if (slow) {
         const float *vt = p.c.vt + ((int64_t)b * Hkv + h) * B * LOCKS_D + c;
 #pragma unroll 1
-        for (int k = 0; full_pages * B + k < min(lim, last); ++k)
+        for (int k = 0; tail_pos + k < min(lim, last - tile0 * kTok); ++k)
 #pragma unroll
           for (int i = 0; i < 32; ++i) {
             const float y = vt[k * LOCKS_D + i];
             if (!(fabsf(y) < INFINITY)) s[i] = f32_bits(__uint_as_float(s[i]) + y);
           }
       }
-      if (real && good) {
+      if (real && good && splits > 1) {
+        float4 *part = reinterpret_cast<float4 *>(p.part + ((int64_t)blockIdx.x * kSoft + tid) * LOCKS_D + c);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          part[i] = make_float4(__uint_as_float(s[4 * i]) * scale, __uint_as_float(s[4 * i + 1]) * scale, __uint_as_float(s[4 * i + 2]) * scale, __uint_as_float(s[4 * i + 3]) * scale);
+      } else if (real && good) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           uint32_t y[4];
@@ -602,7 +652,11 @@ __global__ void __launch_bounds__(kThreads, 1) kvq_chunk_kernel(const __grid_con
         }
       }
     }
-    if (real && good && p.lse) p.lse[row] = l == 0.f ? -INFINITY : ((m == -INFINITY ? 0.f : m) - kTop + log2f(l)) * kLn2;
+    if (real && good) {
+      const float lse2 = l == 0.f ? -INFINITY : (m == -INFINITY ? 0.f : m) - kTop + log2f(l);
+      if (splits > 1) p.part_lse[blockIdx.x * kSoft + tid] = lse2;
+      else if (p.lse) p.lse[row] = lse2 * kLn2;
+    }
     fence_before();
   }
   if (!ok) set_status(p.status, LOCKS_ERR_TIMEOUT);
@@ -614,7 +668,44 @@ __global__ void __launch_bounds__(kThreads, 1) kvq_chunk_kernel(const __grid_con
   }
 }
 
+// Joins the splits of 16 of a block's 256 rows, a warp a row, a lane four dims.
+constexpr int kJoinRows = 16;
+__global__ void __launch_bounds__(32 * kJoinRows) kvq_chunk_join_kernel(const __grid_constant__ ChunkParams p) {
+  __shared__ int found[6];
+  const int lane = threadIdx.x & 31, h = blockIdx.y, G = p.G, cta_tokens = 2 * p.tile_tokens;
+  pdl_trigger();
+  pdl_wait();
+  const int block = blockIdx.x / (kSoft / kJoinRows), r = blockIdx.x % (kSoft / kJoinRows) * kJoinRows + (threadIdx.x >> 5);
+  const Block at = find_block(p, block, 0, found);
+  const int of_half = r % kRows, jr = r / kRows * p.tile_tokens + of_half / G, splits = at.splits;
+  if (at.b < 0 || splits == 1 || of_half >= p.tile_tokens * G || jr >= min(cta_tokens, at.n - at.j0)) return;
+  const int64_t first = ((int64_t)block * p.c.Hkv + h) * splits, row = (int64_t)(at.row0 + jr) * p.Hq + h * G + of_half % G;
+  float m = -INFINITY;
+  for (int s = lane; s < splits; s += 32) m = fmaxf(m, p.part_lse[(first + s) * kSoft + r]);
+  m = warp_max(m);
+  const float ms = m == -INFINITY ? 0.f : m;
+  float sum = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int s = 0; s < splits; ++s) {
+    const float w = ex2f(p.part_lse[(first + s) * kSoft + r] - ms);
+    if (w == 0.f) continue;   // (nothing seen)
+    const float4 y = *reinterpret_cast<const float4 *>(p.part + ((first + s) * kSoft + r) * LOCKS_D + 4 * lane);
+    sum += w;
+    o.x = fmaf(w, y.x, o.x); o.y = fmaf(w, y.y, o.y); o.z = fmaf(w, y.z, o.z); o.w = fmaf(w, y.w, o.w);
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  *reinterpret_cast<uint2 *>(p.out + row * LOCKS_D + 4 * lane) = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+  if (lane == 0 && p.lse) p.lse[row] = sum == 0.f ? -INFINITY : (ms + log2f(sum)) * kLn2;
+}
+
 }  // namespace
+
+// Blocks of 256 rows that `n` tokens of `batch` requests may make, per KV head: most when all requests but one have a single token
+static int64_t chunk_blocks(const locks_ctx *c, int n, int batch) {
+  const int tokens = 2 * (kRows / c->G);
+  return n <= batch ? n : (n - batch) / tokens + batch;
+}
 
 int locks_launch_kvq_chunk(locks_ctx *c, const void *q, const int32_t *cu, int n, const locks_kvq *kv, int batch, void *out, float *lse, cudaStream_t st) {
   ChunkParams p = {};
@@ -624,7 +715,13 @@ int locks_launch_kvq_chunk(locks_ctx *c, const void *q, const int32_t *cu, int n
   p.tile_tokens = kRows / c->G;
   p.log_b = c->B == 64 ? 6 : (c->B == 32 ? 5 : 4);
   p.c2 = c->cfg.sm_scale * kLog2e;
-  const int64_t grid = ((int64_t)n / (2 * p.tile_tokens) + batch) * c->cfg.num_kv_heads;   // a request's last CTA may have fewer rows
+  // Few blocks: the tokens that each sees are split, so that every SM has a share (not where rows, unless they are padding, leave no two
+  // slots for each block)
+  const int64_t blocks = chunk_blocks(c, n, batch), ctas = blocks * c->cfg.num_kv_heads;
+  const int slots = std::min(c->num_sms, KVQ_CHUNK_SLOTS), joined = slots / (2 * c->cfg.num_kv_heads);   // at most so many blocks are split
+  p.slots = ((int64_t)n + 2 * p.tile_tokens - 1) / (2 * p.tile_tokens) <= joined ? slots : 0;
+  p.part = c->kvq_part; p.part_lse = reinterpret_cast<float *>(c->kvq_ml);
+  const int64_t grid = std::max<int64_t>(ctas, p.slots);   // (no slot without a CTA)
   if (grid > INT32_MAX) return LOCKS_ERR_TOO_LARGE;
 #define KVQ_CHUNK(F_)                                                                                                         \
   do {                                                                                                                        \
@@ -635,5 +732,9 @@ int locks_launch_kvq_chunk(locks_ctx *c, const void *q, const int32_t *cu, int n
   if (kv->fmt == LOCKS_KVQ_INT) KVQ_CHUNK(LOCKS_KVQ_INT);
   else KVQ_CHUNK(LOCKS_KVQ_FLOAT);
 #undef KVQ_CHUNK
+  const int rc = locks_check_launch(c);
+  if (rc != LOCKS_OK || !p.slots) return rc;
+  const dim3 rows((unsigned)std::min<int64_t>(blocks, joined) * (kSoft / kJoinRows), c->cfg.num_kv_heads);
+  locks_launch_pdl(kvq_chunk_join_kernel, rows, dim3(32 * kJoinRows), 0, st, p);
   return locks_check_launch(c);
 }
