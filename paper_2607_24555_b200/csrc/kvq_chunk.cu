@@ -10,7 +10,7 @@
 // rows' softmax is under way the tensor cores work for the other 128.
 //
 // Key scales are factors of the scores.  A page's value scale goes into its weights, relative to a power of two that is at least twice
-// the largest value scale so far.  A row's weights are 2^8 p relative to a maximum that may be exceeded by 2^8 before the output is
+// the largest value scale that the row has seen.  A row's weights are 2^8 p relative to a maximum that may be exceeded by 2^8 before the output is
 // rescaled (in tensor memory: rarely more than once or twice a row), so they stay below 2^15, and normal in fp16 down to 2^-20 of the
 // largest.
 //
@@ -18,7 +18,7 @@
 // cores.  Why the scores are read once: a maximum that may be exceeded needs no second pass, and the next 32 columns' maximum hides
 // between these 32's exponentials.  Registers are split by warps' kind (setmaxnreg).  Where blocks of 256 rows are fewer than SMs, the
 // tokens that each sees are shared by several CTAs, and a second kernel joins them.
-// Measured, 1024 tokens of 32 heads over 8 KV heads after 15277: 362 us, 701 TFLOP/s, 0.44 of a library matrix product's rate (with 128 of 148
+// Measured, 1024 tokens of 32 heads over 8 KV heads after 15277: 369 us, 718 TFLOP/s, 0.43 of a library matrix product's rate (with 128 of 148
 // SMs at work: a CTA for each block); without the softmax 252, without products and conversion 276.  Pipes are about half busy
 // (exponentials 50 %, tensor cores 40 %, issue 43 %): bound by the latencies of a chain of softmax and products with two softmax warps a
 // scheduler.  One request's tokens after 16K: 47 us (32 tokens), 73 (128), 205 (512).  Accumulators add up in the tensor cores' fp32.
@@ -509,18 +509,16 @@ __global__ void __launch_bounds__(kThreads, 1) kvq_chunk_kernel(const __grid_con
         }
         tmem_wait_st();
       };
-      // the values' reference
+      // the largest value scale of the pages that this row sees
       const float *ks = ms.scale[stage][0], *vs = ms.scale[stage][1];
-      {
-        float vmax = vs[0];
+      float vmax = 0.f;
+      if (mask) {
 #pragma unroll
-        for (int i = 1; i < kParts; ++i) vmax = fmaxf(vmax, vs[i]);   // (a NaN is not a larger one)
-        if (2.f * vmax > vref) {
-          const uint32_t e = min((f32_bits(vmax) >> 23) + 2u, 252u);
-          inv = __uint_as_float((254u - e) << 23);
-          rescale(vref * inv, 0);
-          vref = __uint_as_float(e << 23);
-        }
+        for (int i = 0; i < kParts; ++i)
+          if (pos + 16 * i < lim && ((there >> i) & 1)) vmax = fmaxf(vmax, vs[i]);   // (a NaN is not a larger one)
+      } else {
+#pragma unroll
+        for (int i = 0; i < kParts; ++i) vmax = fmaxf(vmax, vs[i]);
       }
       // ---- 32 tokens at a time: weights, and between them the maximum of the next 32
       uint32_t buf[2][32];
@@ -567,11 +565,19 @@ __global__ void __launch_bounds__(kThreads, 1) kvq_chunk_kernel(const __grid_con
         for (int i = 0; i < 4; ++i) {
           const uint32_t *s = buf[i & 1];
           const bool up = mx > m + 8.f;   // (also the first that is seen: the row's output and sum are zero then)
-          if (__any_sync(0xffffffffu, up)) {
+          const bool up_v = i == 0 && 2.f * vmax > vref;
+          if (__any_sync(0xffffffffu, up || up_v)) {
             const float to = up ? ceilf(mx) : m, fix = up && m != -INFINITY ? ex2f(m - to) : 1.f;
             sum.x *= fix; sum.y *= fix; l *= fix;
             m = to;
-            rescale(fix, 16 * i);
+            float fix_v = 1.f;
+            if (up_v) {
+              const uint32_t e = min((f32_bits(vmax) >> 23) + 2u, 252u);
+              inv = __uint_as_float((254u - e) << 23);
+              fix_v = vref * inv;
+              vref = __uint_as_float(e << 23);
+            }
+            rescale(fix * fix_v, 16 * i);
           }
           const float off = kTop - (m == -INFINITY ? 0.f : m);
           uint32_t w[16];

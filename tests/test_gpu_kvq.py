@@ -615,3 +615,195 @@ def test_refusals():
             f()
             print("not refused:", i)
     assert ctx.locks_poll_status() == 0
+
+
+# ------------------------------------------------------------------------------------------------ chunks: shares, heads, scales
+@pytest.mark.parametrize("fmt,B,layout", [("int8", 16, "HND"), ("e4m3", 32, "NHD"), ("int8", 64, "HND")])
+@pytest.mark.parametrize("Hq,Hkv,lens,new,pad", [
+    (32, 8, [32], [32], 0),                      # a share per tile, and more shares than tiles
+    (32, 8, [2500], [40], 3),
+    (32, 2, [1201, 700], [25, 24], 0),           # 16 heads a group, a second half of a block with one token
+    (32, 2, [129], [129], 0),
+    (8, 8, [640, 1000], [300, 129], 0),          # one head a group
+    (15, 3, [400, 33, 0, 77], [90, 33, 0, 70], 9),
+    (16, 1, [3001], [64], 200),
+    (32, 8, [100 + 7 * i for i in range(40)], [30 + i % 3 for i in range(40)], 0)])
+def test_attend_chunks_in_shares(Hq, Hkv, lens, new, pad, fmt, B, layout):
+    """Few blocks of rows, so that several CTAs share the tokens of each; more requests than a warp has lanes."""
+    ctx, kvq, q, out, lse = run_attend(Hq, Hkv, B, fmt, layout, lens, new, pad)
+    check_attend(Hq, Hkv, B, lens, new, kvq, q, out, lse)
+    assert ctx.locks_poll_status() == 0
+
+
+@pytest.mark.parametrize("Hkv", [1, 16])
+def test_attend_chunks_take_nothing_of_later_pages(Hkv):
+    """Later pages of the chunk hold far larger values: rows that do not see them lose nothing to them."""
+    lens, new = [256], [256]
+
+    def change(kvq):
+        for p in range(16):
+            kvq.v_scale[kvq.block_table[0, p].long()] *= 2.0 ** (3 * p)
+
+    ctx, kvq, q, out, lse = run_attend(4 * Hkv, Hkv, 16, "int8", "HND", lens, new, change=change)
+    check_attend(4 * Hkv, Hkv, 16, lens, new, kvq, q, out, lse)
+
+
+def test_attend_chunks_scales_of_any_size():
+    lens, new = [700, 190], [100, 60]
+    ctx, kvq, q, out, lse = run_attend(8, 2, 16, "int8", "HND", lens, new, spread=4.0, q_scale=0.01)
+    check_attend(8, 2, 16, lens, new, kvq, q, out, lse)
+
+
+@pytest.mark.parametrize("Hq,Hkv,T,m", [(32, 8, 100_003, 32), (16, 1, 50_016, 90)])
+def test_attend_chunks_of_long_sequences(Hq, Hkv, T, m):
+    """Hundreds of tiles a share, against torch in 64 bits on the GPU."""
+    ctx, kvq, q, out, lse = run_attend(Hq, Hkv, 16, "e4m3", "HND", [T], [m])
+    G, blocks = Hq // Hkv, kvq.block_table[0, :T // 16].long()
+    see = torch.arange(T, device=DEV)[None] < (T - m + 1 + torch.arange(m, device=DEV))[:, None]
+    for h in {0, Hkv - 1}:
+        k, v = [torch.cat([(getattr(kvq, n)[blocks, h].double() * getattr(kvq, n + "_scale")[blocks, h].double()[:, None, None]).flatten(0, 1),
+                           getattr(kvq, n + "_tail")[0, h, :T % 16].double()]) for n in ("k", "v")]
+        s = torch.einsum("mgd,td->mgt", q[:, h * G:h * G + G].double(), k) * 128 ** -0.5
+        s = s.masked_fill(~see[:, None], -math.inf)
+        p = torch.softmax(s, 2)
+        want, ll = p @ v, torch.logsumexp(s, 2)
+        # 2^-8 of the result, 2^-11 of each weight; scores within 2^-16 of their magnitudes, which are below 200
+        tol = 2.0 ** -8 * want.abs() + (2.0 ** -11 + 200 * 2.0 ** -16) * 1.1 * (p @ v.abs()) + 1e-4
+        assert float(((out[:, h * G:h * G + G].double() - want).abs() - tol).max()) <= 0
+        assert float((lse[:, h * G:h * G + G].double() - ll).abs().max()) <= 200 * 2.0 ** -16
+    assert ctx.locks_poll_status() == 0
+
+
+def test_attend_chunks_infinities_and_nan():
+    """An infinite value and a NaN key in the unfinished page reach the rows that see them, and no other; a page whose scale is NaN too."""
+    Hq, Hkv, T, m = 16, 4, 203, 60
+
+    def change(kvq):
+        kvq.v_tail[0, 1, 3, 7] = float("inf")
+        kvq.k_tail[0, 2, 5, 9] = float("nan")
+        kvq.k_scale[int(kvq.block_table[0, 11]), 3] = float("nan")
+
+    ctx, kvq, q, out, lse = run_attend(Hq, Hkv, 16, "int8", "HND", [T], [m], change=change)
+    o, l = out.float(), lse
+    first = T - m                      # row j sees tokens 0 .. first + j
+    tail, page = T // 16 * 16, 11 * 16
+    for j in range(m):
+        g = lambda h: slice(4 * h, 4 * h + 4)
+        assert bool(torch.isfinite(o[j, g(0)]).all())
+        assert bool((o[j, g(1), 7] == float("inf")).all()) == (first + j >= tail + 3)
+        assert bool(torch.isfinite(o[j, g(1), :7]).all() and torch.isfinite(o[j, g(1), 8:]).all() and torch.isfinite(l[j, g(1)]).all())
+        assert bool(torch.isnan(o[j, g(2)]).all()) == (first + j >= tail + 5) and bool(torch.isfinite(o[j, g(2)]).all()) == (first + j < tail + 5)
+        assert bool(torch.isnan(o[j, g(3)]).all()) == (first + j >= page) and bool(torch.isfinite(o[j, g(3)]).all()) == (first + j < page)
+    assert ctx.locks_poll_status() == 0
+
+
+def test_attend_chunks_report_bad_blocks_and_rows():
+    Hq, Hkv = 32, 8
+    ctx, kvq, q, out, lse = run_attend(Hq, Hkv, 16, "int8", "HND", [200, 90], [40, 40])
+    assert ctx.locks_poll_status() == 0
+    # rows that are not there, and a request before them: its rows are answered, those of the other not
+    out.fill_(7.0)
+    ctx.locks_kvq_attend(q, kvq, 2, out, lse, cu_tokens=torch.tensor([0, 40, 100], dtype=torch.int32, device=DEV))
+    assert ctx.locks_poll_status() == -6
+    check_attend(Hq, Hkv, 16, [200], [40], kvq, q[:40], out[:40], lse[:40])
+    assert bool((out[40:] == 7.0).all())
+    # a block outside the cache: none of its tokens are seen
+    kvq.block_table[0, 0] = -3
+    ctx.locks_kvq_attend(q, kvq, 2, out, lse, cu_tokens=U.cu_of([40, 40], DEV))
+    assert ctx.locks_poll_status() == -6 and bool(torch.isfinite(out.float()).all())
+    check_attend(Hq, Hkv, 16, [90], [40], _second(kvq), q[40:], out[40:], lse[40:])
+
+
+def _second(kvq):
+    """The cache as its second request sees it."""
+    import copy
+    one = copy.copy(kvq)
+    one.block_table, one.seq_lens = kvq.block_table[1:], kvq.seq_lens[1:]
+    one.k_tail, one.v_tail = kvq.k_tail[1:], kvq.v_tail[1:]
+    return one
+
+
+# ------------------------------------------------------------------------------------------------ many requests, far rows, repeated pages
+@pytest.mark.parametrize("Hq,Hkv,some", [(8, 2, False), (8, 2, True), (16, 1, True)])
+def test_attend_more_requests_than_lanes(Hq, Hkv, some):
+    lens = [(37 * i) % 150 for i in range(75)]
+    new = [min(t, 1 + (i % 3 if some else 0)) for i, t in enumerate(lens)]
+    if not some:
+        new = [1] * 75
+    ctx, kvq, q, out, lse = run_attend(Hq, Hkv, 16, "int8", "HND", lens, new, 2 if some else 0)
+    check_attend(Hq, Hkv, 16, lens, new, kvq, q, out, lse)
+    assert ctx.locks_poll_status() == 0
+
+
+def test_attend_a_page_listed_twice_counts_twice():
+    lens, k, B = [16 * 20 + 5], 6, 16
+    ids = torch.tensor([[[3, 3, 7, 20, 20, 2], [20, 20, 20, 1, 1, 1]]], dtype=torch.int32)
+    cnt = torch.tensor([[6, 4]], dtype=torch.int32)
+    ctx, kvq, q, out, lse = run_attend(8, 2, B, "int8", "HND", lens, [1], ids=ids.to(DEV), cnt=cnt.to(DEV), budget=k * B)
+    check_attend(8, 2, B, lens, [1], kvq, q, out, lse, ids, cnt)
+    assert ctx.locks_poll_status() == 0
+
+
+@pytest.mark.parametrize("n", [1, 40])
+def test_attend_and_append_far_into_a_large_cache(n):
+    """Blocks beyond 2^32 bytes, and strides that are not the tensors' own order."""
+    Hq, Hkv, B, T, stride = 32, 8, 16, 100, 1 << 26
+    gen = torch.Generator().manual_seed(n)
+    small = U.random_cache(gen, 1, [T], Hkv, B, "int8")
+    nb = 68
+    big = [torch.empty((nb - 1) * stride + Hkv * B * 128, dtype=torch.int8, device=DEV) for _ in range(2)]
+    k, v = [t.as_strided((nb, Hkv, B, 128), (stride, B * 128, 128, 1)) for t in big]
+    table = small.block_table.clone()
+    ks, vs = torch.zeros(nb, Hkv, device=DEV), torch.zeros(nb, Hkv, device=DEV)
+    for p in range(T // B):
+        old, at = int(table[0, p]), nb - 1 - p
+        k[at], v[at], ks[at], vs[at] = small.k[old], small.v[old], small.k_scale[old], small.v_scale[old]
+        table[0, p] = at
+    table[0, T // B] = nb - 1 - T // B
+    kvq = locks.KVQView(k, v, ks, vs, small.k_tail, small.v_tail, table, small.seq_lens)
+    ctx = context(Hq, Hkv, batch=2, pages=table.shape[1])
+    # the page's last tokens, then attention of the last n
+    x, y = rows(gen, 12, Hkv, "bf16"), rows(gen, 12, Hkv, "bf16")
+    kvq.seq_lens.fill_(T + 12)
+    ctx.locks_kvq_append(x, y, kvq, 1, cu_tokens=U.cu_of([12], DEV))
+    q = torch.randn(n, Hq, 128, generator=gen).to(torch.bfloat16).to(DEV)
+    out, lse = torch.empty_like(q), torch.empty(n, Hq, device=DEV)
+    ctx.locks_kvq_attend(q, kvq, 1, out, lse, cu_tokens=U.cu_of([n], DEV))
+    assert float(ks[nb - 1 - T // B].min()) > 0
+    check_attend(Hq, Hkv, B, [T + 12], [n], kvq, q, out, lse)
+    assert ctx.locks_poll_status() == 0
+
+
+def test_appends_of_more_requests_than_threads():
+    """300 requests: lookups that walk the requests in steps."""
+    Hkv, B, batch = 2, 16, 300
+    new = [(7 * i) % 4 for i in range(batch)]
+    lens = [m + (5 * i) % 30 for i, m in enumerate(new)]
+    n = sum(new)
+    gen = torch.Generator().manual_seed(5)
+    k, v = rows(gen, n, Hkv, "bf16"), rows(gen, n, Hkv, "bf16")
+    pages = [-(-t // B) for t in lens]
+    table = torch.full((batch, 3), -1, dtype=torch.int32)
+    at = 0
+    for b, p in enumerate(pages):
+        table[b, :p] = torch.arange(at, at + p)
+        at += p
+    cu = U.cu_of(new, DEV)
+    seq = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    ctx = context(2, Hkv, B=B, batch=batch, pages=3)
+    kc, vc = [torch.zeros(at, Hkv, B, 128, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    kv = KVView(kc, vc, kc.stride()[:3], at, table.to(DEV), seq)
+    ctx.locks_append_rows(k, v, kv, batch, cu_tokens=cu)
+    kvq = new_kvq_cache(at, batch, Hkv, B, table.to(DEV), seq)
+    ctx.locks_kvq_append(k, v, kvq, batch, cu_tokens=cu)
+    assert ctx.locks_poll_status() == 0
+    row = 0
+    for b, (t, m) in enumerate(zip(lens, new)):
+        for j in range(m):
+            pos = t - m + j
+            blk = int(table[b, pos // B])
+            assert torch.equal(kc[blk, :, pos % B], k[row]) and torch.equal(vc[blk, :, pos % B], v[row])
+            if pos >= t // B * B:
+                assert torch.equal(kvq.k_tail[b, :, pos % B], k[row].float()) and torch.equal(kvq.v_tail[b, :, pos % B], v[row].float())
+            row += 1
+    assert row == n
