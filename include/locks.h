@@ -422,13 +422,19 @@ int locks_kvq_append(locks_ctx *ctx, const locks_rotary *rot, const int32_t *pos
                      const locks_kvq *kv, int batch, locks_stream stream);
 
 /* Attention over the 8-bit cache: for every row of q, softmax(q.k_i sm_scale)-weighted mean of v_i.  bf16 configurations.
- *   q            [num_tokens][Hq][d], out likewise, lse optional [num_tokens][Hq] fp32 (natural log)
+ *   q            [num_tokens][Hq][d] bf16, out likewise, both 16-byte aligned and apart; lse optional [num_tokens][Hq] fp32 (natural log)
  *   cu_tokens    NULL: one token per request (num_tokens == batch), which sees its T_b tokens; else as in locks_append_rows, and
  *                token j of request b sees the first T_b - n_b + j + 1 tokens (drafted tokens, a chunk of a prompt)
  *   page_ids     [batch][Hkv][k] and page_count [batch][Hkv], as locks_select writes them (LOCKS_COMBINE_PER_HEAD: one table per
- *                query head), or both NULL: every page.  One token per request only (with cu_tokens: INVALID_ARG).
+ *                query head), or both NULL: every page.  One token per request only (with cu_tokens: INVALID_ARG).  Pages in any
+ *                order; one that is listed twice counts twice.
  * A row that sees nothing gets zeros and a lse of -inf.  Rows behind the last request's are left as they were.  Lengths, counts, page
- * and block ids out of range are reported (LOCKS_ERR_BAD_BLOCK) and skipped. */
+ * and block ids out of range are reported (LOCKS_ERR_BAD_BLOCK) and skipped; rows that no request of the batch can have (cu_tokens out of
+ * 0 .. num_tokens, or descending) are reported and left as they were.  Partial results lie in the context's workspace: calls on one
+ * context that overlap race on it, as locks_select's and locks_sparse_attend's do.
+ * Where cu_tokens is given and rows are many (96 or more per KV head and request on average), queries times weights run on tcgen05
+ * with weights relative to the largest value scale of the pages that a row sees: a page whose values are smaller than that by
+ * more than 2^20 loses precision.  LOCKS_ERR_TOO_LARGE: more rows or pages than a launch can number (beyond 2^31 in all). */
 int locks_kvq_attend(locks_ctx *ctx, const void *q, const int32_t *cu_tokens, int num_tokens, const locks_kvq *kv, int batch,
                      const int32_t *page_ids, const int32_t *page_count, void *out, float *lse, locks_stream stream);
 
