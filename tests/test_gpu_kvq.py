@@ -807,3 +807,53 @@ def test_appends_of_more_requests_than_threads():
                 assert torch.equal(kvq.k_tail[b, :, pos % B], k[row].float()) and torch.equal(kvq.v_tail[b, :, pos % B], v[row].float())
             row += 1
     assert row == n
+
+
+def test_chunks_captured_on_streams_and_between_other_forms():
+    """A captured chunk (append and attention, its tokens shared by several CTAs) replayed with other lengths; token and chunk forms in turn,
+    which use one workspace; two contexts at once, bit for bit."""
+    Hq, Hkv, B, m = 32, 8, 16, 40
+    gen = torch.Generator().manual_seed(11)
+    room, at = [700, 500], [120, 77]
+    kvq = U.random_cache(gen, 2, room, Hkv, B, "e4m3")
+    kvq.seq_lens.copy_(torch.tensor(at, dtype=torch.int32))
+    for n in ("k", "v"):   # (the cache of a sequence of those lengths: its unfinished page in the tail)
+        getattr(kvq, n + "_tail").copy_(torch.randn(2, Hkv, B, 128, generator=gen).to(DEV))
+    ctx = context(Hq, Hkv, B=B, batch=2, pages=kvq.block_table.shape[1], budget=2 * B)
+    rot = make_rotary(freqs(128))
+    cu = U.cu_of([m, m], DEV)
+    q, k, v = rows(gen, 2 * m, Hq, "bf16"), rows(gen, 2 * m, Hkv, "bf16"), rows(gen, 2 * m, Hkv, "bf16")
+    qo, out, lse = torch.empty_like(q), torch.empty_like(q), torch.empty(2 * m, Hq, device=DEV)
+    one, one_lse = torch.empty(2, Hq, 128, dtype=torch.bfloat16, device=DEV), torch.empty(2, Hq, device=DEV)
+
+    def step():
+        ctx.locks_kvq_append(k, v, kvq, 2, rotary=rot, q=q, q_out=qo, cu_tokens=cu)
+        ctx.locks_kvq_attend(qo, kvq, 2, out, lse, cu_tokens=cu)
+        ctx.locks_kvq_attend(qo[:2], kvq, 2, one, one_lse)
+        ctx.locks_kvq_attend(qo, kvq, 2, out, lse, cu_tokens=cu)
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        kvq.seq_lens += m
+        step()
+        with torch.cuda.graph(graph, stream=side):
+            step()
+        for i in range(6):
+            kvq.seq_lens += m
+            for t, h in ((q, Hq), (k, Hkv), (v, Hkv)):
+                t.copy_(rows(gen, 2 * m, h, "bf16"))
+            graph.replay()
+            side.synchronize()
+            now = [t + (2 + i) * m for t in at]
+            check_attend(Hq, Hkv, B, now, [m, m], kvq, qo, out, lse)
+            check_attend(Hq, Hkv, B, now, [1, 1], kvq, qo[:2], one, one_lse)
+    torch.cuda.current_stream().wait_stream(side)
+    ctx2 = context(Hq, Hkv, B=B, batch=2, pages=kvq.block_table.shape[1], budget=2 * B)
+    outs, streams = [torch.empty_like(q) for _ in range(2)], [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for i in range(20):
+        for c, o, s in zip((ctx, ctx2), outs, streams):
+            c.locks_kvq_attend(qo, kvq, 2, o, cu_tokens=cu, stream=s)
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], out) and torch.equal(outs[1], out)
+    assert ctx.locks_poll_status() == 0 and ctx2.locks_poll_status() == 0
