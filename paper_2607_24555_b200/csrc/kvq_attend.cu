@@ -28,6 +28,7 @@ constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kRowPad = LOCKS_D + 4;   // floats of a row of a warp's partial
 constexpr int kUnfinished = -2;        // in a block's place: the unfinished page
 constexpr int kMostLead = 24;          // pairs that a problem's start costs a CTA that has another one's end before it
+constexpr int kTailPairs = 5;           // pairs that a warp reads while another works on an unfinished page (chat traffic 59.5 to 56.6 us, drafts 49.3 to 48)
 constexpr int kMinShare = kWarps;      // places of a share at least: a pair per warp
 constexpr int kJoinWarps = 8;
 constexpr int kManyShares = 16;        // CTAs per problem from which on the partials are put together by a second kernel
@@ -561,15 +562,20 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<NH>) kvq_token_kernel(con
       tiles = npages << p.sub_shift;
     }
     const int lim_min = T - req.n + j0 + 1;   // what the row tile's first token sees
-    // ---- the segment's pairs: this warp's are seg0 + warp + 4 j.  Blocks and scales of 16 pairs at a time, a lane per tile.
-    const int first = seg0 + warp, sub_mask = (1 << p.sub_shift) - 1, end = min(seg1, (tiles + 1) >> 1);
-    const int mine = end > first ? (end - first + kWarps - 1) / kWarps : 0;
+    // ---- the segment's pairs: this warp's are pair_at(j).  Blocks and scales of 16 pairs at a time, a lane per tile.  Where the problem's last
+    // pair, with its unfinished page, is among them, the warp that has it gets kTailPairs fewer than the others.
+    const int sub_mask = (1 << p.sub_shift) - 1, end = min(seg1, (tiles + 1) >> 1), count = max(end - seg0, 0);
+    const int fewer = end == min(req.pairs, (tiles + 1) >> 1) && T & (B - 1) && count ? min(kTailPairs, (count - 1) / (kWarps - 1)) : 0;
+    const int owner = (count - 1 - (kWarps - 1) * fewer) & (kWarps - 1), more = warp == owner ? 0 : fewer;
+    const int first = seg0 + warp - (warp > owner), rest = seg0 + (kWarps - 1) * fewer + warp - kWarps * more;   // (pairs of the first `more` rounds, of the others)
+    auto pair_at = [&](int j) { return j < more ? first + (kWarps - 1) * j : rest + kWarps * j; };
+    const int mine = max((count - (kWarps - 1) * fewer - warp + kWarps - 1) / kWarps, 0) + more;
     struct Batch {
       int blk, page;         // block, page of this lane's tile
       float ks, vs;
       uint32_t have, easy;   // tiles of codes; those among them that every row sees whole.  Not uniform bits of the others: 0
     };
-    auto tile_at = [&](int jb) { return 2 * (first + (jb + (lane >> 1)) * kWarps) + (lane & 1); };
+    auto tile_at = [&](int jb) { return 2 * pair_at(jb + (lane >> 1)) + (lane & 1); };
     auto page_at = [&](int tile) { return p.ids ? p.ids[((int64_t)b * p.Hkv + h) * p.kbud + (tile >> p.sub_shift)] : tile >> p.sub_shift; };
     auto resolve = [&](int jb) {
       const int tile = tile_at(jb);
@@ -608,7 +614,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<NH>) kvq_token_kernel(con
         for (int w = 0; w < 2; ++w) {
           const int bk = __shfl_sync(0xffffffffu, r.blk, l + w);
           if ((r.have >> (l + w)) & 1) {
-            const int sub = (2 * (first + j * kWarps) + w) & sub_mask;
+            const int sub = (2 * pair_at(j) + w) & sub_mask;
             const int64_t off = (int64_t)bk * p.c.sb + (int64_t)hkv * p.c.sh + (int64_t)(sub * 16) * st + c_off;
             const char *kp = p.c.k + off, *vp = p.c.v + off;
 #pragma unroll
@@ -728,7 +734,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<NH>) kvq_token_kernel(con
       } else {
 #pragma unroll 1
         for (int w = 0; w < 2; ++w) {
-          const int sub = (2 * (first + j * kWarps) + w) & sub_mask;
+          const int sub = (2 * pair_at(j) + w) & sub_mask;
           const int pos = __shfl_sync(0xffffffffu, cur.page, l + w) * B + sub * 16;
           if (!((cur.have >> (l + w)) & 1)) {
             if (__shfl_sync(0xffffffffu, cur.blk, l + w) == kUnfinished) tails += 1ull << (16 * sub);
