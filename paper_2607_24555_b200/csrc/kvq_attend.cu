@@ -28,7 +28,7 @@ constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kRowPad = LOCKS_D + 4;   // floats of a row of a warp's partial
 constexpr int kUnfinished = -2;        // in a block's place: the unfinished page
 constexpr int kMostLead = 24;          // pairs that a problem's start costs a CTA that has another one's end before it
-constexpr int kTailPairs = 5;           // pairs that a warp reads while another works on an unfinished page (chat traffic 59.5 to 56.6 us, drafts 49.3 to 48)
+constexpr int kTailPairs = 5;           // pairs that a warp reads while another works on an unfinished page (2 to 5 alike; chat traffic 59.5 to 56.6 us)
 constexpr int kMinShare = kWarps;      // places of a share at least: a pair per warp
 constexpr int kJoinWarps = 8;
 constexpr int kManyShares = 16;        // CTAs per problem from which on the partials are put together by a second kernel
@@ -355,19 +355,21 @@ struct Running {
   }
 };
 
+template <int NH> struct Queries {   // as fragments, and what undoes their power of two, times sm_scale log2 e
+  uint32_t f[NH][8][2];
+  float2 rs[NH];
+};
 // 16 places of the unfinished page (fp32), from pos on, joined to the warp's partial `times` over.  Elements go to fp16 times a power
 // of two of the tile's largest, values rounded (2^-11 of each), keys in two parts.  Out of line: its registers would be the tile loop's.
 template <int NH, int FMT>
-__device__ __noinline__ void tail_tile(const QAttParams &p, int row0, int h, int rows, int T, int2 lim0, int2 lim1, const float *kt, const float *vt, int pos, float times, float *wo, float2 *wml) {
+__device__ __noinline__ void tail_tile(const Queries<NH> &q, int T, int2 lim0, int2 lim1, const float *kt, const float *vt, int pos, float times, float *wo, float2 *wml) {
   const int lane = threadIdx.x & 31, x = lane >> 2, t = lane & 3;
-  uint32_t qf[NH][8][2], pb[1][NH][2];
-  float2 rs[NH], none[NH], f[1][NH];
+  uint32_t pb[1][NH][2];
+  float2 f[1][NH];
   float pw[1][NH][4], s[1][NH][4];
   int2 lim[NH];
   lim[0] = lim0;
   lim[NH - 1] = NH == 1 ? lim0 : lim1;
-  uint4 raw[NH][4];
-  fetch_queries<NH>(p, row0, h, rows, x, t, raw);
   Running<NH> run;
   run.clear();
   float4 k[2][8];
@@ -394,7 +396,6 @@ __device__ __noinline__ void tail_tile(const QAttParams &p, int row0, int h, int
     for (int i = 0; i < 8; ++i)
       amax = fmaxf(amax, fmaxf(fmaxf(finite_abs(k[w][i].x), finite_abs(k[w][i].y)), fmaxf(finite_abs(k[w][i].z), finite_abs(k[w][i].w))));
   float up = power_to(warp_max(amax), 14);
-  take_queries<NH>(p, raw, t, qf, rs, none);
   bool odd = false;   // an infinity or a NaN
 #pragma unroll
   for (int w = 0; w < 2; ++w)
@@ -418,12 +419,12 @@ __device__ __noinline__ void tail_tile(const QAttParams &p, int row0, int h, int
       }
 #pragma unroll
     for (int hh = 0; hh < NH; ++hh) {
-      mma_f16(s[0][hh], a[0], a[1], a[2], a[3], qf[hh][i][0], qf[hh][i][1]);
-      if (finite_tile) mma_f16(s[0][hh], rest[0], rest[1], rest[2], rest[3], qf[hh][i][0], qf[hh][i][1]);
+      mma_f16(s[0][hh], a[0], a[1], a[2], a[3], q.f[hh][i][0], q.f[hh][i][1]);
+      if (finite_tile) mma_f16(s[0][hh], rest[0], rest[1], rest[2], rest[3], q.f[hh][i][0], q.f[hh][i][1]);
     }
   }
 #pragma unroll
-  for (int hh = 0; hh < NH; ++hh) f[0][hh] = make_float2(rs[hh].x / up, rs[hh].y / up);
+  for (int hh = 0; hh < NH; ++hh) f[0][hh] = make_float2(q.rs[hh].x / up, q.rs[hh].y / up);
   run.template weights<1, true>(s, f, lim, pos, x, pb, pw);
   amax = 0.f;
   odd = false;
@@ -701,7 +702,14 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<NH>) kvq_token_kernel(con
         run.outputs(2 * w + 1, ha[2][0], ha[3][0], ha[2][1], ha[3][1], pb, from, fv);
       }
     };
-    uint64_t tails = 0;   // times that each 16-token part of the unfinished page is listed, 16 bits a part
+    // times that this warp takes each 16-token part of the unfinished page, 16 bits a part: where all pages are read, the parts that lie
+    // in the segment go to different warps, the owner's first; of a page table, the parts that the warp meets
+    uint64_t tails = 0;
+    if (!p.ids && T & (B - 1) && full_pages < p.c.Pmax)
+      for (int sub = 0; sub * 16 < (T & (B - 1)); ++sub) {
+        const int pair = ((full_pages << p.sub_shift) + sub) >> 1;
+        if (pair >= seg0 && pair < end && ((owner + sub) & (kWarps - 1)) == warp) tails += 1ull << (16 * sub);
+      }
 #pragma unroll 1
     for (int j = 0; j < mine; ++j) {
       const int jn = j + S - 1, l = 2 * (j & 15);
@@ -737,7 +745,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<NH>) kvq_token_kernel(con
           const int sub = (2 * pair_at(j) + w) & sub_mask;
           const int pos = __shfl_sync(0xffffffffu, cur.page, l + w) * B + sub * 16;
           if (!((cur.have >> (l + w)) & 1)) {
-            if (__shfl_sync(0xffffffffu, cur.blk, l + w) == kUnfinished) tails += 1ull << (16 * sub);
+            if (p.ids && __shfl_sync(0xffffffffu, cur.blk, l + w) == kUnfinished) tails += 1ull << (16 * sub);
             continue;
           }
           float s[1][NH][4], pw[1][NH][4];
@@ -765,7 +773,14 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<NH>) kvq_token_kernel(con
     for (int sub = 0; tails; ++sub, tails >>= 16) {
       if (!(tails & 0xffff)) continue;
       const int64_t at = (((int64_t)b * kv_heads + hkv) * B + 16 * sub) * LOCKS_D;
-      tail_tile<NH, FMT>(p, req.row0 + j0, h, rows, T, lim[0], lim[NH - 1], p.c.kt + at, p.c.vt + at, full_pages * B + 16 * sub, (float)(tails & 0xffff), part_of(warp), ml_of(warp));
+      Queries<NH> q;   // (a copy: what a call takes by address lies in memory)
+#pragma unroll
+      for (int hh = 0; hh < NH; ++hh) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { q.f[hh][i][0] = qf[hh][i][0]; q.f[hh][i][1] = qf[hh][i][1]; }
+        q.rs[hh] = FMT == LOCKS_KVQ_INT ? make_float2(rs[hh].x * 0x1p-24f, rs[hh].y * 0x1p-24f) : rs[hh];
+      }
+      tail_tile<NH, FMT>(q, T, lim[0], lim[NH - 1], p.c.kt + at, p.c.vt + at, full_pages * B + 16 * sub, (float)(tails & 0xffff), part_of(warp), ml_of(warp));
       __syncwarp();
     }
     __syncthreads();

@@ -857,3 +857,29 @@ def test_chunks_captured_on_streams_and_between_other_forms():
     torch.cuda.synchronize()
     assert torch.equal(outs[0], out) and torch.equal(outs[1], out)
     assert ctx.locks_poll_status() == 0 and ctx2.locks_poll_status() == 0
+
+
+@pytest.mark.parametrize("new", [[1, 1], [3, 2]])
+def test_attend_takes_no_unfinished_page_behind_the_table(new):
+    """A length beyond an odd row of the table is reported; the pages that are there are attended, the unfinished one is not."""
+    Hq, Hkv, B, pages = 8, 2, 16, 5
+    lens = [pages * B + 7, 40]
+    gen = torch.Generator().manual_seed(2)
+    kvq = U.random_cache(gen, 2, lens, Hkv, B, "int8", rows_more=0)
+    kvq.block_table = kvq.block_table[:, :pages].contiguous()
+    ctx = context(Hq, Hkv, B=B, batch=2, pages=pages, budget=2 * B)
+    n = sum(new)
+    q = torch.randn(n, Hq, 128, generator=gen).to(torch.bfloat16).to(DEV)
+    out, lse = torch.empty_like(q), torch.empty(n, Hq, device=DEV)
+    ctx.locks_kvq_attend(q, kvq, 2, out, lse, cu_tokens=U.cu_of(new, DEV) if n > 2 else None)
+    assert ctx.locks_poll_status() == -6
+    # every row of the first request sees its 80 tokens in pages
+    k, v, _ = U.sequence(kvq, 0, 0, pages * B, B)
+    k1, v1, _ = U.sequence(kvq, 0, 1, pages * B, B)
+    for h, (kk, vv) in enumerate(((k, v), (k1, v1))):
+        s = U.f64(q[:new[0], 4 * h:4 * h + 4]) @ kk.T * 128 ** -0.5
+        want, ll = torch.softmax(s, -1) @ vv, torch.logsumexp(s, -1)
+        # 2^-8 of the result, 2^-11 of each weight; scores within 2^-16 of their magnitudes, which are below 100; 17 x 255 x 2^-23 of a scale (below 0.1)
+        tol = 2.0 ** -8 * want.abs() + (2.0 ** -11 + 100 * 2.0 ** -16) * 1.1 * (torch.softmax(s, -1) @ vv.abs()) + 17 * 255 * 2.0 ** -23 * 0.1
+        near(out[:new[0], 4 * h:4 * h + 4], want, tol, "out")
+        near(lse[:new[0], 4 * h:4 * h + 4], ll, torch.full_like(ll, 100 * 2.0 ** -16), "lse")
