@@ -60,6 +60,9 @@ __global__ void __launch_bounds__(kExWarps * 32) exact_bf16_kernel(ExactParams p
   const int chunk = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
   uint8_t *ring = smem + warp * kExStages * kExTile;
   const uint8_t *Kb = reinterpret_cast<const uint8_t *>(p.k);
+  const float c2 = p.sm_scale * kLog2e;
+  pdl_wait();   // lengths, and queries that a rotation or an append may just have written
+  const int T = p.seq_lens[b];
   // query as the B operand: lane (x, t) holds head x (+8), dims 16 s + 2t.. and 16 s + 8 + 2t..
   uint32_t qb[NH][8][2];
   {
@@ -70,14 +73,11 @@ __global__ void __launch_bounds__(kExWarps * 32) exact_bf16_kernel(ExactParams p
       const uint32_t *qr = reinterpret_cast<const uint32_t *>(q + ((int64_t)b * p.Hq + h * p.G + g) * LOCKS_D);
 #pragma unroll
       for (int s = 0; s < 8; ++s) {
-        qb[hh][s][0] = (g < p.G) ? __ldg(qr + 8 * s + t) : 0u;
-        qb[hh][s][1] = (g < p.G) ? __ldg(qr + 8 * s + 4 + t) : 0u;
+        qb[hh][s][0] = (g < p.G) ? qr[8 * s + t] : 0u;
+        qb[hh][s][1] = (g < p.G) ? qr[8 * s + 4 + t] : 0u;
       }
     }
   }
-  const float c2 = p.sm_scale * kLog2e;
-  pdl_wait();
-  const int T = p.seq_lens[b];
   const int P = (T + LOCKS_B - 1) / LOCKS_B;
   const int lo = chunk * kExPagesPerCta, hi = min(lo + kExPagesPerCta, P);
   // this warp's pages: lo + warp + 4 j, j < 16; lane j resolves page j's block

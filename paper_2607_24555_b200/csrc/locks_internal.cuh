@@ -171,7 +171,8 @@ int locks_launch_fake_quant(locks_ctx *c, const locks_kv *kv, int batch, const i
 
 // Launch with programmatic dependent launch allowed: the kernel may be scheduled while its stream
 // predecessor is still draining; it must execute pdl_wait() before touching anything the predecessor
-// writes (the wait returns once the predecessor grid has completed and its writes are visible).
+// writes (the wait returns once the predecessor grid has completed and its writes are visible): every buffer of the caller is such, since
+// rotations and appends write queries and the cache and start their successors at once.
 template <typename... KArgs, typename... Args>
 static inline void locks_launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st,
                                     Args... args) {

@@ -356,7 +356,7 @@ __device__ __forceinline__ void mma_f16_z(float (&d)[4], uint32_t a0, uint32_t a
 __device__ __forceinline__ void fetch_q_row(const __nv_bfloat16 *row, int t, bool valid, uint4 (&v)[4]) {
   const uint4 *qp = reinterpret_cast<const uint4 *>(row + 32 * t);
 #pragma unroll
-  for (int m = 0; m < 4; ++m) v[m] = valid ? __ldg(qp + m) : make_uint4(0u, 0u, 0u, 0u);
+  for (int m = 0; m < 4; ++m) v[m] = valid ? qp[m] : make_uint4(0u, 0u, 0u, 0u);
 }
 __device__ __forceinline__ void load_q_row(const uint4 (&v)[4], uint32_t (&a0)[8], uint32_t (&a2)[8], float &inv, float &sum8) {
   const uint32_t *w = reinterpret_cast<const uint32_t *>(v);
@@ -1151,7 +1151,7 @@ __device__ __forceinline__ void load_q_row_exact(const __nv_bfloat16 *row, int t
   if (valid) {
     const uint4 *qp = reinterpret_cast<const uint4 *>(row + 32 * t);
 #pragma unroll
-    for (int m = 0; m < 4; ++m) v[m] = __ldg(qp + m);
+    for (int m = 0; m < 4; ++m) v[m] = qp[m];
   }
   const uint32_t *w = reinterpret_cast<const uint32_t *>(v);
   uint32_t mx = 0u;  // largest |q| of the row as a bf16 bit pattern (orders like the value)
