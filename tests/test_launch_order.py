@@ -57,3 +57,19 @@ def test_every_kernel_that_may_start_early_waits_before_it_reads():
 def test_nothing_is_read_by_the_non_coherent_path():
     for f, t in sources().items():
         assert "__ldg(" not in t and "ld.global.nc" not in t, f
+
+
+def test_tensor_memory_is_reached_by_whole_warps():
+    """Tensor-memory loads and stores (and numbered barriers) are executed by all lanes of a warp together: wherever the chunk form
+    branches by lane, the lanes come together before the next of them."""
+    t = " ".join(sources()["kvq_chunk.cu"].split())
+    for start in ("auto rescale = [&](float fix, int columns) {",                         # called where some row's maximum rose
+                  "for (int c = 0; c < LOCKS_D; c += 32) { uint32_t s[32];",              # results: rows differ in what is not finite
+                  "if (lane == 0) ms.red[8 * kv + warp - 8] = y; }"):
+        at = t.index(start) + len(start)
+        assert t[at:].lstrip().startswith("__syncwarp();"), start
+    # where rows differ in what they see of a tile
+    assert "decltype(masked_)::value; if (kMasked) __syncwarp();" in t and "if (kMasked) __syncwarp(); tmem_st<16>(w, " in t
+    assert "if (part == 1 && i < 3) { if (kMasked) __syncwarp(); tmem_wait_ld();" in t
+    assert re.search(r"if \(warp == 16\) \{ __syncwarp\(\); asm volatile\(\"tcgen05\.alloc", t)
+    assert re.search(r"__syncwarp\(\); fence_after\(\); asm volatile\(\"tcgen05\.dealloc", t)
