@@ -430,7 +430,8 @@ int locks_kvq_append(locks_ctx *ctx, const locks_rotary *rot, const int32_t *pos
  *                order; one that is listed twice counts twice.
  * A row that sees nothing gets zeros and a lse of -inf.  Rows behind the last request's are left as they were.  Lengths, counts, page
  * and block ids out of range are reported (LOCKS_ERR_BAD_BLOCK) and skipped; rows that no request of the batch can have (cu_tokens out of
- * 0 .. num_tokens, or descending) are reported and left as they were.  Partial results lie in the context's workspace: calls on one
+ * 0 .. num_tokens, or descending) are reported and left as they were, and so are all rows if such offsets give them to several requests
+ * so often that there are more than batch + num_tokens tiles of them.  Partial results lie in the context's workspace: calls on one
  * context that overlap race on it, as locks_select's and locks_sparse_attend's do.
  * Where cu_tokens is given and rows are many (96 or more per KV head and request on average), queries times weights run on tcgen05
  * with weights relative to the largest value scale of the pages that a row sees: a page whose values are smaller than that by

@@ -108,7 +108,7 @@ __device__ __forceinline__ int scan_places(int mine, int lane) {
 }
 
 // The line as a warp knows it: the first 32 requests (most batches: all), its length and the CTAs' share of it.  (The host sees to it
-// that the length fits 32 bits.)  A problem's pairs come after `lead` places that stand for what its start costs: its queries, first
+// that the length fits 32 bits; all: 0 where the offsets are such that it does not.)  A problem's pairs come after `lead` places that stand for what its start costs: its queries, first
 // blocks and tiles, and joining its warps' partials take a CTA some 10 us, as long as 24 pairs do.  Without them a CTA with two
 // problems in its share ends that much later (24 requests of 211 .. 9001 tokens, 8 heads: 76 us; 6 places 66, 24 places 51).  A quarter of
 // the share at most: where shares are short every CTA has a start of its own, and places without work would leave CTAs idle.
@@ -119,15 +119,21 @@ struct Line {
   __device__ __forceinline__ void read(const QAttParams &p, int lane, int ctas) {
     r = Request{0, 0, 0, 0, 0};
     if (lane < p.batch) r = request_at(p, lane);
-    int pairs = __reduce_add_sync(0xffffffffu, r.pairs * r.row_tiles), problems = __reduce_add_sync(0xffffffffu, r.row_tiles);
-    for (int b0 = 32; b0 < p.batch; b0 += 32) {
+    int pairs = __reduce_add_sync(0xffffffffu, r.pairs * r.row_tiles);
+    const uint32_t most = (uint32_t)p.batch + (uint32_t)p.n;   // row tiles at most, which the host has counted with
+    uint32_t problems = __reduce_add_sync(0xffffffffu, (uint32_t)r.row_tiles);
+    for (int b0 = 32; b0 < p.batch && problems <= most; b0 += 32) {
       Request x = {0, 0, 0, 0, 0};
       if (b0 + lane < p.batch) x = request_at(p, b0 + lane);
       pairs += __reduce_add_sync(0xffffffffu, x.pairs * x.row_tiles);
-      problems += __reduce_add_sync(0xffffffffu, x.row_tiles);
+      problems += __reduce_add_sync(0xffffffffu, (uint32_t)x.row_tiles);
+    }
+    if (problems > most) {   // offsets that do not ascend give rows to several requests: a longer line than 32 bits may hold
+      set_status(p.status, LOCKS_ERR_BAD_BLOCK);
+      pairs = problems = 0;
     }
     lead = min(pairs * p.Hkv / (4 * ctas), kMostLead);
-    all = (pairs + lead * problems) * p.Hkv;
+    all = (pairs + lead * (int)problems) * p.Hkv;
     share = max((all - 1) / ctas + 1, kMinShare);
     end = scan_places(places(p, r), lane);
   }
@@ -855,6 +861,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) kvq_join_kernel(const __grid_
   if (j >= req.n) return;   // (offsets out of range)
   Line line;
   line.read(p, lane, ctas);
+  if (line.all == 0) return;
   const int share = line.share;
   int before = 0;   // places of the requests before
   if (b < 32) {
