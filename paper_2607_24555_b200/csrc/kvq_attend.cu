@@ -2,7 +2,8 @@
 //   o_r = sum_i softmax_i(q_r . k_i s_k(i) sm_scale) v_i s_v(i)   over the tokens i that row r sees.
 //
 // Codes are numbers that fp16 holds exactly, so both products run on the tensor cores in fp16.  A query row goes in times a power of
-// two that brings its largest element to 1 .. 2 (exact, and undone on the scores in fp32), a page's key scale is a factor of its
+// two that brings its largest element to 1 .. 2 (undone on the scores in fp32; elements down to 2^-17 of the largest go in exactly, smaller
+// ones within 2^-25 of it, which is where fp16 ends), a page's key scale is a factor of its
 // scores, and P V of 16 tokens joins the fp32 output by one rounding multiply-add with the page's value scale, so that no scale meets
 // fp16's range.  Weights go in as 2^15 p in fp16 (within 2^-11 of each, and normal down to p = 2^-29); the sum that divides is that of
 // the unrounded ones.  Scores, maxima, sums and outputs are fp32.
@@ -210,17 +211,20 @@ __device__ __forceinline__ void take_queries(const QAttParams &p, const uint4 (&
     const float up = power_to(amax, 0);
     const float back = p.c2 / up;
     rs[hh] = make_float2(__shfl_sync(0xffffffffu, back, 8 * t), __shfl_sync(0xffffffffu, back, 8 * t + 4));
-    float sum = 0.f;
+    float sum = 0.f;   // of the elements as the products take them
 #pragma unroll
     for (int s = 0; s < 8; ++s)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sum += v[s][e] * up;
+      for (int e = 0; e < 2; ++e) {
+        qf[hh][s][e] = pack_f16(v[s][2 * e] * up, v[s][2 * e + 1] * up);
+        const float2 y = __half22float2(*reinterpret_cast<const __half2 *>(&qf[hh][s][e]));
+        sum += y.x;
+        sum += y.y;
+      }
     sum += __shfl_xor_sync(0xffffffffu, sum, 1);
     sum += __shfl_xor_sync(0xffffffffu, sum, 2);
     sum *= -0x1p-17f;
     start[hh] = make_float2(__shfl_sync(0xffffffffu, sum, 8 * t), __shfl_sync(0xffffffffu, sum, 8 * t + 4));
-#pragma unroll
-    for (int s = 0; s < 8; ++s) { qf[hh][s][0] = pack_f16(v[s][0] * up, v[s][1] * up); qf[hh][s][1] = pack_f16(v[s][2] * up, v[s][3] * up); }
   }
 }
 

@@ -62,3 +62,51 @@ def _request(kvq, b):
     one.block_table, one.seq_lens = kvq.block_table[b:], kvq.seq_lens[b:]
     one.k_tail, one.v_tail = kvq.k_tail[b:], kvq.v_tail[b:]
     return one
+
+
+# ------------------------------------------------------------------------------------------------ queries whose elements differ much in size
+# What fp16 queries may move a score by: every element within 2^-25 of its row's largest, times the sum of a key's magnitudes.
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("Hq,Hkv,new", [(8, 2, 1), (16, 1, 1), (8, 2, 3), (64, 16, 100)])
+def test_attend_query_elements_below_the_largest(Hq, Hkv, new, fmt):
+    """One large element that meets codes of zero, and 127 of 0.97 x 2^-25 of it: scores are the small ones' alone, the same to within their
+    rounding whatever a page's scale is.  (Signed codes are multiplied as code + 128: what that adds has to be taken off as the products have it.)"""
+    T, B, gen = 128, 16, torch.Generator().manual_seed(7)
+    kvq = U.random_cache(gen, 1, [T], Hkv, B, fmt)
+    codes = torch.randint(-1, 2, kvq.k.shape, generator=gen).float()
+    codes[..., 0] = 0
+    kvq.k.copy_(codes.to(kvq.k.dtype).to(DEV))
+    kvq.k_scale.copy_((2.0 ** torch.randint(0, 3, kvq.k_scale.shape, generator=gen)).to(DEV))
+    ctx = context(Hq, Hkv, B=B, batch=1, pages=kvq.block_table.shape[1])
+    q = torch.full((new, Hq, 128), 2.0 ** 16 * 0.96875 * 2.0 ** -25)
+    q[..., 0] = 2.0 ** 16
+    q = q.to(torch.bfloat16).to(DEV)
+    out, lse = torch.empty_like(q), torch.empty(new, Hq, device=DEV)
+    ctx.locks_kvq_attend(q, kvq, 1, out, lse, cu_tokens=U.cu_of([new], DEV))
+    wo, wl, bo, bl = U.attend(q, kvq, [T], [new], Hkv, B)
+    more = 2.0 ** -25 * 2.0 ** 16 * 127 * 4 * 128 ** -0.5   # (codes -1 .. 1, scales up to 4)
+    assert more < 0.1
+    vmax = max(float(U.sequence(kvq, 0, h, T, B)[1].abs().max()) for h in range(Hkv))
+    near(out, wo, bo + 2 * math.expm1(more) * vmax, "out")
+    near(lse, wl, bl + more, "lse")
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("Hq,Hkv,lens,new", [(8, 2, [300, 47], [1, 1]), (16, 1, [200], [2]), (64, 16, [210, 333], [90, 140])])
+def test_attend_query_elements_of_all_sizes(Hq, Hkv, lens, new, fmt):
+    """Elements of a row spread over 2^-30 .. 1."""
+    gen = torch.Generator().manual_seed(8)
+    kvq = U.random_cache(gen, len(lens), lens, Hkv, 16, fmt)
+    ctx = context(Hq, Hkv, batch=len(lens), pages=kvq.block_table.shape[1])
+    n = sum(new)
+    q = (4.0 * torch.randn(n, Hq, 128, generator=gen) * 2.0 ** (-30 * torch.rand(n, Hq, 128, generator=gen))).to(torch.bfloat16).to(DEV)
+    out, lse = torch.empty_like(q), torch.empty(n, Hq, device=DEV)
+    ctx.locks_kvq_attend(q, kvq, len(lens), out, lse, cu_tokens=U.cu_of(new, DEV))
+    wo, wl, bo, bl = U.attend(q, kvq, lens, new, Hkv, 16)
+    kmax = max(float(U.sequence(kvq, b, h, t, 16)[0].abs().sum(-1).max()) for b, t in enumerate(lens) for h in range(Hkv))
+    vmax = max(float(U.sequence(kvq, b, h, t, 16)[1].abs().max()) for b, t in enumerate(lens) for h in range(Hkv))
+    more = 2.0 ** -25 * float(U.f64(q).abs().max()) * kmax * 128 ** -0.5
+    assert more < 1e-3
+    near(out, wo, bo + 2 * math.expm1(more) * vmax, "out")
+    near(lse, wl, bl + more, "lse")
+    assert ctx.locks_poll_status() == 0
