@@ -41,7 +41,7 @@ def test_attend_offsets_that_go_back(Hq, Hkv, n):
     """A request whose offsets descend is reported and has no rows; those of the others are answered.  Both forms."""
     lens = [350, 40, 333]
     kvq = U.random_cache(torch.Generator().manual_seed(3), 3, lens, Hkv, 16, "int8")
-    ctx = context(Hq, Hkv, batch=3, pages=kvq.block_table.shape[1])
+    ctx = context(Hq, Hkv, batch=3, pages=kvq.block_table.shape[1], budget=128)
     q = torch.randn(2 * n, Hq, 128, generator=torch.Generator().manual_seed(4)).to(torch.bfloat16).to(DEV)
     out, lse = torch.full_like(q, 7.0), torch.full((2 * n, Hq), 7.0, device=DEV)
     cu = torch.tensor([0, n, n - 2, 2 * n - 2], dtype=torch.int32, device=DEV)
@@ -77,7 +77,7 @@ def test_attend_query_elements_below_the_largest(Hq, Hkv, new, fmt):
     codes[..., 0] = 0
     kvq.k.copy_(codes.to(kvq.k.dtype).to(DEV))
     kvq.k_scale.copy_((2.0 ** torch.randint(0, 3, kvq.k_scale.shape, generator=gen)).to(DEV))
-    ctx = context(Hq, Hkv, B=B, batch=1, pages=kvq.block_table.shape[1])
+    ctx = context(Hq, Hkv, B=B, batch=1, pages=kvq.block_table.shape[1], budget=128)
     q = torch.full((new, Hq, 128), 2.0 ** 16 * 0.96875 * 2.0 ** -25)
     q[..., 0] = 2.0 ** 16
     q = q.to(torch.bfloat16).to(DEV)
@@ -97,7 +97,7 @@ def test_attend_query_elements_of_all_sizes(Hq, Hkv, lens, new, fmt):
     """Elements of a row spread over 2^-30 .. 1."""
     gen = torch.Generator().manual_seed(8)
     kvq = U.random_cache(gen, len(lens), lens, Hkv, 16, fmt)
-    ctx = context(Hq, Hkv, batch=len(lens), pages=kvq.block_table.shape[1])
+    ctx = context(Hq, Hkv, batch=len(lens), pages=kvq.block_table.shape[1], budget=128)
     n = sum(new)
     q = (4.0 * torch.randn(n, Hq, 128, generator=gen) * 2.0 ** (-30 * torch.rand(n, Hq, 128, generator=gen))).to(torch.bfloat16).to(DEV)
     out, lse = torch.empty_like(q), torch.empty(n, Hq, device=DEV)
@@ -110,3 +110,135 @@ def test_attend_query_elements_of_all_sizes(Hq, Hkv, lens, new, fmt):
     near(out, wo, bo + 2 * math.expm1(more) * vmax, "out")
     near(lse, wl, bl + more, "lse")
     assert ctx.locks_poll_status() == 0
+
+
+# ------------------------------------------------------------------------------------------------ long sequences, page by page
+def marked_cache(gen, lens, Hkv, B, fmt, layout):
+    """Every page has scales of its own; keys have a code of one in dimension 0 (which alone the queries have), values one in the
+    dimension that the page's number gives.  So a page that is lost, taken twice or taken with another's scale shows."""
+    batch, pages = len(lens), [-(-t // B) for t in lens]
+    nb = sum(pages)
+    order = torch.randperm(nb, generator=gen, device=DEV).to(torch.int32)
+    table = torch.full((batch, max(pages) + 1), 1 << 30, dtype=torch.int32, device=DEV)
+    at = 0
+    for b, p in enumerate(pages):
+        table[b, :p] = order[at:at + p]
+        at += p
+    kvq = new_kvq_cache(nb, batch, Hkv, B, table, torch.tensor(lens, dtype=torch.int32, device=DEV), fmt=fmt, layout=layout)
+    for s, lo in ((kvq.k_scale, 0.5), (kvq.v_scale, 0.5)):
+        s.copy_(lo * 4.0 ** torch.rand(s.shape, generator=gen, device=DEV))
+    kvq.k[..., 0] = torch.ones(1, device=DEV).to(kvq.k.dtype)
+    for b, p in enumerate(pages):
+        v = torch.zeros(p, Hkv, B, 128, device=DEV)
+        v[torch.arange(p, device=DEV), :, :, torch.arange(p, device=DEV) % 128] = 1.0
+        kvq.v[table[b, :p].long()] = v.to(kvq.v.dtype)
+        del v
+        last = lens[b] // B
+        kvq.k_tail[b, :, :, 0] = 0.75
+        kvq.v_tail[b, :, :, last % 128] = 1.25
+    return kvq
+
+
+def marked_answer(kvq, b, h, T, B, a, pages, sees):
+    """64 bits: (mean of values, log of the weights' sum) for queries a in dimension 0 over `pages` in that order, a row with `sees` tokens."""
+    whole = T // B
+    blocks = kvq.block_table[b, pages.clamp(max=whole)].long().clamp(0, kvq.k.shape[0] - 1)
+    ks = torch.where(pages < whole, kvq.k_scale[blocks, h].double(), 0.75)
+    vs = torch.where(pages < whole, kvq.v_scale[blocks, h].double(), 1.25)
+    count = (sees - pages * B).clamp(0, B).double()
+    w = torch.exp(a[:, None].double() * ks * 128 ** -0.5) * count
+    total = w.sum(1)
+    out = torch.zeros(len(a), 128, dtype=torch.float64, device=DEV).index_add_(1, pages % 128, w * vs) / total[:, None]
+    return out, torch.log(total)
+
+
+def check_marked(got, lse, want, ll, fmt, what):
+    """A score is one product (exact) times a row's and a page's factor (|s| <= 0.5; four roundings: 2^-23), its exponential within 2^-22, and
+    a sum is of at most 256 numbers one after the other, and as many partials (2^-15): 2^-14 in all; a page of 16 tokens among 10^5 is 2^-13 to 2^-12.
+    Outputs are rounded (2^-8) as weights are (2^-11; with the value's scale, once more); signed codes: 17 x 255 x 2^-23 of a scale (up to 2)."""
+    assert float((lse.double() - ll).abs().max()) <= 2.0 ** -14, what
+    tol = want.abs() * (2.0 ** -8 + 2.0 ** -10 + 2.0 ** -13) + (17 * 255 * 2.0 ** -23 * 2 if fmt == "int8" else 0.0) + 1e-6
+    assert float(((got.double() - want).abs() - tol).max()) <= 0, what
+
+
+def marked_queries(n, Hq):
+    q = torch.zeros(n, Hq, 128, dtype=torch.bfloat16, device=DEV)
+    q[..., 0] = (2.8 * (0.3 + 0.7 * torch.arange(Hq, device=DEV) / Hq) * (1 - 2 * (torch.arange(Hq, device=DEV) % 2))).to(torch.bfloat16)
+    return q
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("Hq,Hkv,B,layout,lens", [
+    (32, 8, 16, "HND", [32_005, 31_000, 29_999, 32_768, 30_001, 8_200, 25_000, 16_384]),
+    (32, 2, 16, "NHD", [60_003, 59_000, 61_111, 33, 64_000, 50_050, 60_000, 62_001, 40_000, 47_007]),
+    (8, 2, 32, "NHD", [61_005, 60_000, 59_000, 44, 1, 60_032, 55_555, 32_768, 64_001, 63_000, 50_000, 61_000, 60_001, 60_002, 60_003, 50_001]),
+    (8, 4, 64, "HND", [61_005, 60_000, 59_000, 60_032, 55_555, 32_768, 64_001, 30_000])])
+def test_attend_every_page_of_long_sequences(Hq, Hkv, B, layout, lens, fmt):
+    """Warps with many batches of blocks and scales: tens of pairs of tiles each."""
+    gen = torch.Generator(device=DEV).manual_seed(sum(lens))
+    kvq = marked_cache(gen, lens, Hkv, B, fmt, layout)
+    batch, G = len(lens), Hq // Hkv
+    ctx = context(Hq, Hkv, B=B, batch=batch, pages=kvq.block_table.shape[1], budget=128)
+    q = marked_queries(batch, Hq)
+    out, lse = torch.full_like(q, 7.0), torch.full((batch, Hq), 7.0, device=DEV)
+    ctx.locks_kvq_attend(q, kvq, batch, out, lse)
+    assert ctx.locks_poll_status() == 0
+    for b, t in enumerate(lens):
+        pages = torch.arange(-(-t // B), device=DEV)
+        for h in range(Hkv):
+            heads = slice(h * G, h * G + G)
+            want, ll = marked_answer(kvq, b, h, t, B, q[b, heads, 0], pages, t)
+            check_marked(out[b, heads], lse[b, heads], want, ll, fmt, (b, h))
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("per_head", [False, True])
+def test_attend_every_listed_page(fmt, per_head):
+    """A thousand pages of each head in any order, the unfinished one among them."""
+    Hq, Hkv, B, k, lens = 32, 8, 16, 1024, [40_005, 33_000, 20_000, 31_111, 16_390, 30_000, 28_001, 17_000]
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    kvq = marked_cache(gen, lens, Hkv, B, fmt, "HND")
+    batch, G, tables = len(lens), Hq // Hkv, Hq if per_head else Hkv
+    more = {"combine": locks.COMBINE_PER_HEAD} if per_head else {}
+    ctx = context(Hq, Hkv, B=B, batch=batch, pages=kvq.block_table.shape[1], budget=k * B, **more)
+    ids = torch.zeros(batch, tables, k, dtype=torch.int32, device=DEV)
+    cnt = torch.full((batch, tables), k, dtype=torch.int32, device=DEV)
+    for b, t in enumerate(lens):
+        pages = -(-t // B)
+        for h in range(tables):
+            ids[b, h] = torch.randperm(pages - 1, generator=gen, device=DEV)[:k].to(torch.int32)
+            ids[b, h, (7 * h + b) % k] = pages - 1
+            cnt[b, h] = k - (h * b) % 50
+    q = marked_queries(batch, Hq)
+    out, lse = torch.full_like(q, 7.0), torch.full((batch, Hq), 7.0, device=DEV)
+    ctx.locks_kvq_attend(q, kvq, batch, out, lse, page_ids=ids, page_count=cnt)
+    assert ctx.locks_poll_status() == 0
+    for b, t in enumerate(lens):
+        for i in range(tables):
+            heads = slice(i, i + 1) if per_head else slice(i * G, i * G + G)
+            pages = ids[b, i, :int(cnt[b, i])].long()
+            want, ll = marked_answer(kvq, b, i // G if per_head else i, t, B, q[b, heads, 0], pages, t)
+            check_marked(out[b, heads], lse[b, heads], want, ll, fmt, (b, i))
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("Hq,Hkv,B,lens,new", [(32, 8, 16, [100_003], [32]), (32, 8, 16, [40_000, 30_005], [300, 299]), (64, 16, 32, [50_001, 7_000, 22_222], [64, 64, 40]),
+                                               (16, 1, 64, [90_016], [60]), (32, 8, 16, [50_005, 60_000], [3, 2])])
+def test_chunks_attend_every_page_of_long_sequences(Hq, Hkv, B, lens, new, fmt):
+    gen = torch.Generator(device=DEV).manual_seed(sum(lens))
+    kvq = marked_cache(gen, lens, Hkv, B, fmt, "HND")
+    batch, G, n = len(lens), Hq // Hkv, sum(new)
+    ctx = context(Hq, Hkv, B=B, batch=batch, pages=kvq.block_table.shape[1], budget=128)
+    q = marked_queries(n, Hq)
+    out, lse = torch.full_like(q, 7.0), torch.full((n, Hq), 7.0, device=DEV)
+    ctx.locks_kvq_attend(q, kvq, batch, out, lse, cu_tokens=U.cu_of(new, DEV))
+    assert ctx.locks_poll_status() == 0
+    row = 0
+    for b, (t, m) in enumerate(zip(lens, new)):
+        pages = torch.arange(-(-t // B), device=DEV)
+        for j in {0, 1, m // 2, m - 1}:
+            for h in {0, Hkv // 2, Hkv - 1}:
+                heads = slice(h * G, h * G + G)
+                want, ll = marked_answer(kvq, b, h, t, B, q[row + j, heads, 0], pages, t - m + j + 1)
+                check_marked(out[row + j, heads], lse[row + j, heads], want, ll, fmt, (b, j, h))
+        row += m
