@@ -428,8 +428,10 @@ int locks_kvq_append(locks_ctx *ctx, const locks_rotary *rot, const int32_t *pos
  *   page_ids     [batch][Hkv][k] and page_count [batch][Hkv], as locks_select writes them (LOCKS_COMBINE_PER_HEAD: one table per
  *                query head), or both NULL: every page.  One token per request only (with cu_tokens: INVALID_ARG).  Pages in any
  *                order; one that is listed twice counts twice.
- * A row that sees nothing gets zeros and a lse of -inf.  Rows behind the last request's are left as they were.  Lengths, counts, page
- * and block ids out of range are reported (LOCKS_ERR_BAD_BLOCK) and skipped; rows that no request of the batch can have (cu_tokens out of
+ * A row that sees nothing gets zeros and a lse of -inf; so do all rows of a request whose length is zero or below (which is not
+ * reported, as in locks_sparse_attend).  Rows behind the last request's are left as they were.  Lengths beyond the block-table row, counts,
+ * page ids outside the row and block ids outside the cache are reported (LOCKS_ERR_BAD_BLOCK) and skipped; a listed page behind the
+ * sequence's last one holds nothing; rows that no request of the batch can have (cu_tokens out of
  * 0 .. num_tokens, or descending) are reported and left as they were, and so are all rows if such offsets give them to several requests
  * so often that there are more than batch + num_tokens tiles of them.  Partial results lie in the context's workspace: calls on one
  * context that overlap race on it, as locks_select's and locks_sparse_attend's do.

@@ -78,7 +78,7 @@ __device__ __forceinline__ Request request_at(const QAttParams &p, int b) {
   Request r;
   r.row0 = b;
   r.n = 1;
-  r.T = p.c.seq_lens[b];
+  r.T = max(p.c.seq_lens[b], 0);   // (a length below zero: an empty sequence)
   if (p.cu) {
     r.row0 = p.cu[b];
     r.n = p.cu[b + 1] - r.row0;

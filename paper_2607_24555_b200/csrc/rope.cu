@@ -374,11 +374,12 @@ __global__ void __launch_bounds__(kQThreads, 2) kvq_append_kernel(const __grid_c
     if (found_s[0] < 0) return;
     b = found_s[0]; item = found_s[1]; row0 = found_s[2]; n = found_s[3];
   }
-  const int T = p.cu ? found_s[4] : c.seq_lens[b], start = T - n;
-  if (start < 0 || T > kMostTokens) {   // (one token per request: none at a length of zero)
+  const int T = p.cu ? found_s[4] : c.seq_lens[b];
+  if (T < n || T > kMostTokens) {   // (one token per request: none at a length of zero)
     if (tid == 0 && T != 0) set_status(a.status, LOCKS_ERR_BAD_BLOCK);
     return;
   }
+  const int start = T - n;
   const int sub_shift = B == 64 ? 2 : (B == 32 ? 1 : 0);   // a page is 2^sub_shift warps' work
   auto do_page = [&](int page) {
     const int first = page * B, t0 = max(first, start), t1 = min(first + B, T);

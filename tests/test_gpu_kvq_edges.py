@@ -242,3 +242,33 @@ def test_chunks_attend_every_page_of_long_sequences(Hq, Hkv, B, lens, new, fmt):
                 want, ll = marked_answer(kvq, b, h, t, B, q[row + j, heads, 0], pages, t - m + j + 1)
                 check_marked(out[row + j, heads], lse[row + j, heads], want, ll, fmt, (b, j, h))
         row += m
+
+
+# ------------------------------------------------------------------------------------------------ lengths
+@pytest.mark.parametrize("Hq,Hkv,new", [(8, 2, [1, 1, 1]), (8, 2, [3, 2, 4]), (64, 16, [100, 120, 90])])
+@pytest.mark.parametrize("length", [0, -1, -7, -16, -2 ** 31])
+def test_attend_empty_and_negative_lengths(Hq, Hkv, new, length):
+    """A sequence with nothing in it: zeros and -inf, whatever is in its tail, and nothing of it in the others' rows."""
+    lens = [200, 0, 133]
+    kvq = U.random_cache(torch.Generator().manual_seed(6), 3, lens, Hkv, 16, "int8")
+    kvq.k_tail[1] = kvq.v_tail[1] = float("nan")
+    kvq.seq_lens[1] = length
+    ctx = context(Hq, Hkv, batch=3, pages=kvq.block_table.shape[1])
+    n = sum(new)
+    q = torch.randn(n, Hq, 128, generator=torch.Generator().manual_seed(7)).to(torch.bfloat16).to(DEV)
+    out, lse = torch.full_like(q, 7.0), torch.full((n, Hq), 7.0, device=DEV)
+    ctx.locks_kvq_attend(q, kvq, 3, out, lse, cu_tokens=None if n == 3 else U.cu_of(new, DEV))
+    assert ctx.locks_poll_status() == 0
+    check_attend(Hq, Hkv, 16, lens, new, kvq, q, out, lse)
+
+
+def test_append_of_negative_lengths():
+    """A new token that no length counts: reported, and nothing is written; a length of zero has no new token."""
+    for length, status in ((0, 0), (-1, -6), (-2 ** 31, -6)):
+        kvq = new_kvq_cache(6, 2, 2, 16, torch.arange(6, dtype=torch.int32, device=DEV).view(2, 3), torch.tensor([length, 16], dtype=torch.int32, device=DEV))
+        ctx = context(4, 2, batch=2, pages=3)
+        k = torch.randn(2, 2, 128, generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).to(DEV)
+        ctx.locks_kvq_append(k, k, kvq, 2)
+        assert ctx.locks_poll_status() == status
+        used = [int(x) for x in (kvq.k_scale.abs().sum(1) > 0).nonzero()[:, 0]]
+        assert used == [3] and not bool(kvq.k_tail[0].any())
