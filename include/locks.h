@@ -400,9 +400,16 @@ int locks_append_rows(locks_ctx *ctx, const locks_rotary *rot, const int32_t *po
  * A page whose largest magnitude is below 2^-100 is stored as zeros with a scale of zero; one with an infinity or a NaN gets a
  * scale of NaN and codes of zero: whatever attends it is NaN.  Scales are fp32.
  * Only complete pages are in codes.  The unfinished last page of the request in row b of the batch is kept as it comes, in fp32, in
- * k_tail / v_tail [max_batch][Hkv][page_size][head_dim], and is quantised once, when its last token comes; so the codes do not
- * depend on how a sequence was cut into appends.  A request that moves to another row takes its tail along; a block may
- * be shared as in any paged cache. */
+ * k_tail / v_tail [max_batch][Hkv][tail_pages * page_size][head_dim] (page p in the tail's page p % tail_pages), and is quantised once,
+ * when its last token comes; so the codes do not depend on how a sequence was cut into appends.  A request that moves to
+ * another row takes its tail along; a block may be shared as in any paged cache.
+ * Shorter sequences (drafted tokens that are refused): seq_lens[b] may be set back, and the next append goes on from there.  Let M be the
+ * longest that the sequence has been; attention and appends need the unfinished page's rows in the tail, so T_b may fall
+ *   tail_pages 1   to M / page_size * page_size: not into a page that has been completed.  For that, keep a copy of the row's tails from before
+ *                  the append that completed it, put it back, and append the tokens that stay once more;
+ *   tail_pages 2   to (M / page_size - 1) * page_size: into the last page that has been completed, too.
+ * Below that the rows are gone, which nothing can see: no status is set.  A page's codes are written anew when it is completed anew (and a
+ * summary of it is the caller's to build again). */
 #define LOCKS_KVQ_INT 0
 #define LOCKS_KVQ_FLOAT 1
 typedef struct {
@@ -413,6 +420,7 @@ typedef struct {
   float *k_tail, *v_tail;                           /* 16-byte aligned */
   const int32_t *block_table;                       /* [max_batch][max_pages_per_seq] */
   const int32_t *seq_lens;                          /* [max_batch] */
+  int32_t tail_pages;                               /* pages of a request's tail: 0 or 1: one; 2 */
 } locks_kvq;
 
 /* locks_append_rows for the 8-bit cache.  bf16 configurations (else UNSUPPORTED), pages of 16, 32 and 64 tokens.  cu_tokens has to

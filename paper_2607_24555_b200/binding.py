@@ -56,7 +56,7 @@ class KVQ(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("stride_block", C.c_int64), ("stride_head", C.c_int64),
                 ("stride_token", C.c_int64), ("num_blocks", C.c_int32), ("fmt", C.c_int32), ("k_scale", C.c_void_p),
                 ("v_scale", C.c_void_p), ("k_tail", C.c_void_p), ("v_tail", C.c_void_p), ("block_table", C.c_void_p),
-                ("seq_lens", C.c_void_p)]
+                ("seq_lens", C.c_void_p), ("tail_pages", C.c_int32)]
 
 
 class Rows(C.Structure):
@@ -235,7 +235,8 @@ def _need(ok, what):
 @dataclass
 class KVQView:
     """A paged cache in 8 bits.  k, v: [block, head, token, dim] int8 or float8_e4m3fn tensors (views of any layout whose dims are
-    contiguous); k_scale, v_scale: [block, head] fp32; k_tail, v_tail: [max_batch, head, page_size, dim] fp32."""
+    contiguous); k_scale, v_scale: [block, head] fp32; k_tail, v_tail: [max_batch, head, page_size, dim] fp32, or with twice as many tokens:
+    then a sequence may be shortened by a page (see include/locks.h)."""
     k: torch.Tensor
     v: torch.Tensor
     k_scale: torch.Tensor
@@ -252,7 +253,9 @@ class KVQView:
         for t in (self.k_scale, self.v_scale):
             _need(t.dtype == f32 and t.shape == k.shape[:2] and t.is_contiguous(), "KVQView: scales are contiguous fp32 [block, head]")
         for t in (self.k_tail, self.v_tail):
-            _need(t.dtype == f32 and t.dim() == 4 and t.shape[1:] == k.shape[1:] and t.is_contiguous(), "KVQView: tails are contiguous fp32 [max_batch, head, page_size, dim]")
+            _need(t.dtype == f32 and t.dim() == 4 and t.shape[1] == k.shape[1] and t.shape[2] in (k.shape[2], 2 * k.shape[2]) and t.shape[3] == k.shape[3] and t.is_contiguous(),
+                  "KVQView: tails are contiguous fp32 [max_batch, head, page_size or twice that, dim]")
+        _need(self.k_tail.shape[2] == self.v_tail.shape[2], "KVQView: tails of one size")
         _need(self.block_table.dtype == i32 and self.block_table.dim() == 2 and self.block_table.is_contiguous(), "KVQView: block_table is contiguous int32 [max_batch, max_pages]")
         _need(self.seq_lens.dtype == i32 and self.seq_lens.dim() == 1 and self.seq_lens.is_contiguous(), "KVQView: seq_lens is contiguous int32 [max_batch]")
         _need(all(t.device == k.device for t in (v, self.k_scale, self.v_scale, self.k_tail, self.v_tail, self.block_table, self.seq_lens)), "KVQView: tensors on different devices")
@@ -261,15 +264,20 @@ class KVQView:
         sb, sh, st, _ = self.k.stride()
         return KVQ(self.k.data_ptr(), self.v.data_ptr(), sb, sh, st, self.k.shape[0], KVQ_INT if self.k.dtype == torch.int8 else KVQ_FLOAT,
                    self.k_scale.data_ptr(), self.v_scale.data_ptr(), self.k_tail.data_ptr(), self.v_tail.data_ptr(),
-                   self.block_table.data_ptr(), self.seq_lens.data_ptr())
+                   self.block_table.data_ptr(), self.seq_lens.data_ptr(), self.tail_pages)
+
+    @property
+    def tail_pages(self) -> int:
+        return self.k_tail.shape[2] // self.k.shape[2]
 
     def kv_view(self) -> "KVView":
         """For locks_select and locks_scan, which read the block table and the lengths only."""
         return KVView(self.k, self.v, self.k.stride()[:3], self.k.shape[0], self.block_table, self.seq_lens)
 
 
-def new_kvq_cache(num_blocks, max_batch, Hkv, page_size, block_table, seq_lens, fmt="int8", layout="HND") -> KVQView:
-    """An empty 8-bit cache on the table's device; layout "HND" [block, head, token, dim] or "NHD" [block, token, head, dim] in memory."""
+def new_kvq_cache(num_blocks, max_batch, Hkv, page_size, block_table, seq_lens, fmt="int8", layout="HND", tail_pages=1) -> KVQView:
+    """An empty 8-bit cache on the table's device; layout "HND" [block, head, token, dim] or "NHD" [block, token, head, dim] in memory.
+    tail_pages=2: sequences may be shortened by a page (drafted tokens that are refused; see include/locks.h)."""
     dev, d = block_table.device, 128
     dt = {"int8": torch.int8, "e4m3": torch.float8_e4m3fn}[fmt]
 
@@ -281,8 +289,8 @@ def new_kvq_cache(num_blocks, max_batch, Hkv, page_size, block_table, seq_lens, 
     def f32(*shape):
         return torch.zeros(*shape, dtype=torch.float32, device=dev)
 
-    return KVQView(codes(), codes(), f32(num_blocks, Hkv), f32(num_blocks, Hkv), f32(max_batch, Hkv, page_size, d),
-                   f32(max_batch, Hkv, page_size, d), block_table, seq_lens)
+    return KVQView(codes(), codes(), f32(num_blocks, Hkv), f32(num_blocks, Hkv), f32(max_batch, Hkv, tail_pages * page_size, d),
+                   f32(max_batch, Hkv, tail_pages * page_size, d), block_table, seq_lens)
 
 
 @dataclass

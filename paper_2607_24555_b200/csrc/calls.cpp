@@ -145,19 +145,22 @@ locks_kvq kvq_view(const Context &c, PyObject *o, int batch, const char *call) {
        "codes have to be [block, head, token, 128] of the configuration's heads and page size, dims contiguous, keys and values laid out alike");
   need(kc.scalar_type() == vc.scalar_type() && (kc.scalar_type() == at::kChar || kc.scalar_type() == at::kFloat8_e4m3fn), call, "codes have to be int8 or float8_e4m3fn");
   float *scale[2], *tail[2];
+  int64_t tail_rows = 0;
   PyObject *so[2] = {ks.o, vs.o}, *to[2] = {kt.o, vt.o};
   for (int i = 0; i < 2; ++i) {
     const at::Tensor &s = on(c, so[i], call, "scales"), &t = on(c, to[i], call, "tails");
     need(s.scalar_type() == at::kFloat && s.dim() == 2 && s.size(0) == kc.size(0) && s.size(1) == c.Hkv && s.is_contiguous(), call, "scales have to be contiguous fp32 [block, head]");
-    need(t.scalar_type() == at::kFloat && t.dim() == 4 && t.size(0) >= batch && t.size(1) == c.Hkv && t.size(2) == c.B && t.size(3) == 128 && t.is_contiguous(), call,
-         "tails have to be contiguous fp32 [max_batch, head, page_size, 128]");
+    need(t.scalar_type() == at::kFloat && t.dim() == 4 && t.size(0) >= batch && t.size(1) == c.Hkv && (t.size(2) == c.B || t.size(2) == 2 * c.B) && t.size(3) == 128 && t.is_contiguous(), call,
+         "tails have to be contiguous fp32 [max_batch, head, page_size or twice that, 128]");
+    need(i == 0 || t.size(2) == tail_rows, call, "tails of keys and values have to be of one size");
+    tail_rows = t.size(2);
     scale[i] = s.data_ptr<float>();
     tail[i] = t.data_ptr<float>();
   }
   const at::Tensor &table = on(c, tb.o, call, "block_table"), &lens = on(c, sl.o, call, "seq_lens");
   table_ok(c, table, lens, batch, call);
   return locks_kvq{kc.data_ptr(), vc.data_ptr(), kc.stride(0), kc.stride(1), kc.stride(2), (int32_t)kc.size(0), kc.scalar_type() == at::kChar ? LOCKS_KVQ_INT : LOCKS_KVQ_FLOAT,
-                   scale[0], scale[1], tail[0], tail[1], table.data_ptr<int32_t>(), lens.data_ptr<int32_t>()};
+                   scale[0], scale[1], tail[0], tail[1], table.data_ptr<int32_t>(), lens.data_ptr<int32_t>(), (int32_t)(tail_rows / c.B)};
 }
 
 void check(int rc, const char *call) {

@@ -16,13 +16,19 @@ struct KvqCache {   // the 8-bit cache as the kernels take it
   int64_t sb, sh, st;
   float *ks, *vs, *kt, *vt;
   const int32_t *block_table, *seq_lens;
-  int num_blocks, Hkv, Pmax, B;
+  int num_blocks, Hkv, Pmax, B, tail_pages;
+#ifdef __CUDACC__
+  // first element of the tail's page that `page` of request b has, of KV head h
+  __device__ __forceinline__ int64_t tail_at(int b, int h, int page) const {
+    return ((((int64_t)b * Hkv + h) * tail_pages + (page & (tail_pages - 1))) * B) * LOCKS_D;
+  }
+#endif
 };
 
 static inline KvqCache kvq_cache(const locks_ctx *c, const locks_kvq *kv) {
   return KvqCache{reinterpret_cast<char *>(kv->k), reinterpret_cast<char *>(kv->v), kv->stride_block, kv->stride_head, kv->stride_token,
                   kv->k_scale, kv->v_scale, kv->k_tail, kv->v_tail, kv->block_table, kv->seq_lens, kv->num_blocks,
-                  c->cfg.num_kv_heads, c->Pmax, c->B};
+                  c->cfg.num_kv_heads, c->Pmax, c->B, kv->tail_pages == 2 ? 2 : 1};
 }
 
 static inline int kvq_check(const locks_ctx *c, const locks_kvq *kv, int batch) {
@@ -31,6 +37,7 @@ static inline int kvq_check(const locks_ctx *c, const locks_kvq *kv, int batch) 
   if (c->cfg.kv_dtype != LOCKS_BF16) return LOCKS_ERR_UNSUPPORTED;
   if (batch <= 0 || batch > c->cfg.max_batch || kv->num_blocks <= 0) return LOCKS_ERR_INVALID_ARG;
   if (kv->fmt != LOCKS_KVQ_INT && kv->fmt != LOCKS_KVQ_FLOAT) return LOCKS_ERR_INVALID_ARG;
+  if (kv->tail_pages < 0 || kv->tail_pages > 2) return LOCKS_ERR_INVALID_ARG;
   if (kv->stride_block <= 0 || kv->stride_head <= 0 || kv->stride_token < LOCKS_D) return LOCKS_ERR_INVALID_ARG;
   if ((kv->stride_block | kv->stride_head | kv->stride_token) % 16) return LOCKS_ERR_INVALID_ARG;
   if (((uintptr_t)kv->k | (uintptr_t)kv->v | (uintptr_t)kv->k_tail | (uintptr_t)kv->v_tail) % 16) return LOCKS_ERR_INVALID_ARG;

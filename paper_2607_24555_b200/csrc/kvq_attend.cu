@@ -785,7 +785,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<NH>) kvq_token_kernel(con
 #pragma unroll 1
     for (int sub = 0; tails; ++sub, tails >>= 16) {
       if (!(tails & 0xffff)) continue;
-      const int64_t at = (((int64_t)b * kv_heads + hkv) * B + 16 * sub) * LOCKS_D;
+      const int64_t at = p.c.tail_at(b, hkv, full_pages) + 16 * sub * LOCKS_D;
       Queries<NH> q;   // (a copy: what a call takes by address lies in memory)
 #pragma unroll
       for (int hh = 0; hh < NH; ++hh) {

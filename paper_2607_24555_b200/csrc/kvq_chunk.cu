@@ -360,7 +360,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvq_chunk_kernel(const __grid_con
         // a thread: 32 dims of one token of 64, as fp16 times a power of two of the 64 tokens' largest; keys in two parts (22 bits), the
         // second in rows 64 on; values' rows 64 on are zero
         const int tt = ct >> 2, d0 = 32 * (ct & 3);
-        const int64_t at = (((int64_t)b * Hkv + h) * B + tt) * LOCKS_D + d0;
+        const int64_t at = p.c.tail_at(b, h, full_pages) + tt * LOCKS_D + d0;
         const float *src[2] = {p.c.kt + at, p.c.vt + at};
         const bool in = full_pages * B + tt < T;
         float amax[2] = {0.f, 0.f}, up[2];
@@ -642,7 +642,7 @@ __global__ void __launch_bounds__(kThreads, 1) kvq_chunk_kernel(const __grid_con
         for (int i = 0; i < 32; ++i) s[i] = 0;
       }
       if (slow) {
-        const float *vt = p.c.vt + ((int64_t)b * Hkv + h) * B * LOCKS_D + c;
+        const float *vt = p.c.vt + p.c.tail_at(b, h, full_pages) + c;
 #pragma unroll 1
         for (int k = 0; tail_pos + k < min(lim, last - tile0 * kTok); ++k)
 #pragma unroll

@@ -381,9 +381,11 @@ __global__ void __launch_bounds__(kQThreads, 2) kvq_append_kernel(const __grid_c
   }
   const int start = T - n;
   const int sub_shift = B == 64 ? 2 : (B == 32 ? 1 : 0);   // a page is 2^sub_shift warps' work
-  auto do_page = [&](int page) {
+  const int p0 = start / B, last = T / B;
+  // keep: a page's rows into the tail, and nothing else
+  auto do_page = [&](int page, bool keep) {
     const int first = page * B, t0 = max(first, start), t1 = min(first + B, T);
-    const bool complete = first + B <= T;
+    const bool complete = !keep && first + B <= T;
     const int tasks = 2 * c.Hkv, per_round = kQWarps >> sub_shift, sub = warp & ((1 << sub_shift) - 1), at0 = first + 16 * sub + (lane >> 3);
     auto row_at = [&](int task, int pos) {
       const bool key = !(task & 1);
@@ -424,7 +426,7 @@ __global__ void __launch_bounds__(kQThreads, 2) kvq_append_kernel(const __grid_c
       if (EARLY && r) fetch(r + (warp >> sub_shift));
       const int task = r + (warp >> sub_shift), h = task >> 1;
       const bool live = task < tasks, key = !(task & 1);
-      float *tail = (key ? c.kt : c.vt) + (((int64_t)b * c.Hkv + h) * B) * LOCKS_D;
+      float *tail = (key ? c.kt : c.vt) + c.tail_at(b, h, page);
       float x[4][16];
       float top = 0.f;
       if (live) {
@@ -482,7 +484,9 @@ __global__ void __launch_bounds__(kQThreads, 2) kvq_append_kernel(const __grid_c
           }
           if (lane == 0 && sub == 0) (key ? c.ks : c.vs)[(int64_t)block * c.Hkv + h] = scale;
         }
-      } else if (live && fits) {
+      }
+      // (a page that is complete keeps its rows where the tail has two pages, so that the sequence may be shortened into it)
+      if (live && fits && (!complete || (c.tail_pages == 2 && page == p0 && page == last - 1))) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int pos = at0 + 4 * i;
@@ -491,11 +495,19 @@ __global__ void __launch_bounds__(kQThreads, 2) kvq_append_kernel(const __grid_c
       }
     }
   };
-  const int p0 = start / B, last = T / B;
-  do_page(p0 + item);
-  if (item == 0 && last != p0 && T % B) {
+  if (!EARLY) {   // a single token: its page, and none behind it that has tokens
+    do_page(p0, false);
+    return;
+  }
+  bool keep = false;
+#pragma unroll 1
+  for (int page = p0 + item;;) {
+    do_page(page, keep);
+    if (item || last == p0) break;
+    if (c.tail_pages == 2 && page == p0 && last - 1 != p0) { page = last - 1; keep = true; }
+    else if (page != last && T % B) { page = last; keep = false; }
+    else break;
     __syncthreads();   // the tail's old tokens have been read, the cosines used
-    do_page(last);
   }
 }
 

@@ -83,3 +83,16 @@ def test_library_refuses_bad_arguments_without_a_context():
     assert L.locks_kvq_append(None, None, None, None, 1, None, None, C.byref(rows), C.byref(rows), None, 1, None) == -1
     assert L.locks_kvq_attend(None, None, None, 1, None, 1, None, None, None, None, None) == -1
     assert L.locks_kvq_build_summaries(None, None, 1, None, None, None, None) == -1
+
+
+def test_tails_of_one_or_two_pages():
+    for pages in (1, 2):
+        v = cpu_view(tail_pages=pages)
+        assert v.k_tail.shape == (2, 2, 16 * pages, 128) and v.tail_pages == pages and v.struct().tail_pages == pages
+    two, one = cpu_view(tail_pages=2), cpu_view()
+    parts = dict(k=two.k, v=two.v, k_scale=two.k_scale, v_scale=two.v_scale, block_table=two.block_table, seq_lens=two.seq_lens)
+    with pytest.raises(locks.LocksError, match="one size"):
+        locks.KVQView(k_tail=two.k_tail, v_tail=one.v_tail, **parts)
+    three = torch.zeros(2, 2, 48, 128)
+    with pytest.raises(locks.LocksError, match="twice"):
+        locks.KVQView(k_tail=three, v_tail=three, **parts)
