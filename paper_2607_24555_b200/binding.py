@@ -5,12 +5,14 @@ from __future__ import annotations
 import ctypes as C
 import importlib.util
 import os
+import sys
 from dataclasses import dataclass
 
 import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "liblocks.so")
+_CALLS_PATH = os.path.join(_HERE, "_calls.so")
 
 F32, BF16 = 0, 1
 FMT_F32, FMT_I4, FMT_I8, FMT_BF16 = 0, 1, 2, 3
@@ -147,13 +149,26 @@ def lib():
     return _lib
 
 
+def calls_path() -> str:
+    return _CALLS_PATH
+
+
+def calls_stamp() -> str:
+    """What _calls.so was compiled for, which it has as a string in it: it takes torch's tensors by their C++ classes."""
+    return f"locks calls: torch {torch.__version__}, python {sys.version_info[0]}.{sys.version_info[1]}."
+
+
 def calls():
-    """The native marshalling module (_calls.so, built in-tree with the library), bound to the library's functions."""
+    """The native marshalling module (_calls.so, built in-tree beside the library), bound to the library's functions.  Loaded when a call
+    first takes it."""
     global _calls_module
     if _calls_module is None:
-        path = os.path.join(_HERE, "_calls.so")
+        path = calls_path()
         if not os.path.exists(path):
             raise LocksError(f"{path} is missing: run `python -m paper_2607_24555_b200.build`")
+        with open(path, "rb") as f:
+            if calls_stamp().encode() not in f.read():
+                raise LocksError(f"{path} was built for another torch or Python than torch {torch.__version__}: run `python -m paper_2607_24555_b200.build`")
         spec = importlib.util.spec_from_file_location(__package__ + "._calls", path)
         m = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(m)
@@ -329,13 +344,21 @@ class Context:
             h = C.c_void_p()
             _check(L.locks_create(C.byref(cfg), base, nbytes, C.byref(h)), "locks_create")
         self.handle = h
-        self._calls = calls()
-        self._call = self._calls.context(h.value, cfg.num_q_heads, cfg.num_kv_heads, cfg.max_batch, cfg.max_pages_per_seq, cfg.page_size, self.k,
-                                         self.device.index, cfg.combine == COMBINE_PER_HEAD, self.summary_bytes, cfg.q_dtype == BF16)
+
+    def __getattr__(self, name):   # the native call layer, made by the first call that takes it
+        if name not in ("_calls", "_call"):
+            raise AttributeError(f"{type(self).__name__!r} object has no attribute {name!r}")
+        if not self.__dict__.get("handle"):
+            raise LocksError("the context is closed")
+        cfg, m = self.cfg, calls()
+        self._call = m.context(self.handle.value, cfg.num_q_heads, cfg.num_kv_heads, cfg.max_batch, cfg.max_pages_per_seq, cfg.page_size, self.k,
+                               self.device.index, cfg.combine == COMBINE_PER_HEAD, self.summary_bytes, cfg.q_dtype == BF16)
+        self._calls = m
+        return self.__dict__[name]
 
     def close(self):
-        if self.handle:
-            if getattr(self, "_call", None) is not None:
+        if self.__dict__.get("handle"):
+            if "_call" in self.__dict__:
                 self._calls.close(self._call)
             lib().locks_destroy(self.handle)
             self.handle = None

@@ -12,6 +12,9 @@
 
 #include "locks.h"
 
+// what this module was compiled for: binding.py looks for it in the file before it loads it
+extern "C" __attribute__((used, visibility("default"))) const char locks_calls_stamp[] = LOCKS_CALLS_STAMP;
+
 namespace {
 
 struct Context {

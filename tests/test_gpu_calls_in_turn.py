@@ -142,3 +142,19 @@ def test_many_layers_in_one_graph():
             for l, o in zip(layers, got):
                 assert torch.equal(l.out, o), turn
     torch.cuda.current_stream().wait_stream(side)
+
+
+def test_contexts_do_without_the_native_call_layer(monkeypatch, tmp_path):
+    from paper_2607_24555_b200 import binding
+    monkeypatch.setattr(binding, "_CALLS_PATH", str(tmp_path / "_calls.so"))
+    monkeypatch.setattr(binding, "_calls_module", None)
+    layer = Layer(8, 2, 16, 2, 100, 64, fill_summaries=True)
+    layer.qo.copy_(layer.q)
+    layer.step()
+    torch.cuda.synchronize()
+    assert layer.ctx.locks_poll_status() == 0 and bool(torch.isfinite(layer.out.float()).all())
+    with pytest.raises(locks.LocksError, match="missing"):
+        layer.rope()
+    layer.ctx.close()
+    with pytest.raises(locks.LocksError, match="closed"):
+        layer.rope()
