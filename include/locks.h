@@ -450,7 +450,8 @@ int locks_kvq_attend(locks_ctx *ctx, const void *q, const int32_t *cu_tokens, in
                      const int32_t *page_ids, const int32_t *page_count, void *out, float *lse, locks_stream stream);
 
 /* locks_build_summaries from the codes: the summaries of complete pages of the 8-bit cache, which locks_select then scores
- * (locks_select and locks_scan read block_table and seq_lens of their locks_kv only).  bf16 configurations. */
+ * (locks_select, locks_scan, locks_select_scored and locks_selection_quality read num_blocks, block_table and seq_lens of their locks_kv
+ * only; the calls that read its keys or values take rows of kv_dtype, not codes).  bf16 configurations. */
 int locks_kvq_build_summaries(locks_ctx *ctx, const locks_kvq *kv, int batch, const int32_t *page_begin, const int32_t *page_end,
                               void *summaries, locks_stream stream);
 

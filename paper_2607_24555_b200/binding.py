@@ -286,8 +286,9 @@ class KVQView:
         return self.k_tail.shape[2] // self.k.shape[2]
 
     def kv_view(self) -> "KVView":
-        """For locks_select and locks_scan, which read the block table and the lengths only."""
-        return KVView(self.k, self.v, self.k.stride()[:3], self.k.shape[0], self.block_table, self.seq_lens)
+        """For locks_select, locks_scan, locks_select_scored and locks_selection_quality, which read the block table and the lengths only;
+        calls that read the cache refuse it (codes are half as long as the rows that they would take)."""
+        return TableView(self.k, self.v, self.k.stride()[:3], self.k.shape[0], self.block_table, self.seq_lens)
 
 
 def new_kvq_cache(num_blocks, max_batch, Hkv, page_size, block_table, seq_lens, fmt="int8", layout="HND", tail_pages=1) -> KVQView:
@@ -322,6 +323,17 @@ class KVView:
         sb, sh, st = self.strides
         return KV(self.k.data_ptr(), self.v.data_ptr(), sb, sh, st, self.num_blocks, self.block_table.data_ptr(),
                   self.seq_lens.data_ptr())
+
+    def tables(self) -> KV:
+        """For calls that read no keys and values."""
+        return KVView.struct(self)
+
+
+class TableView(KVView):
+    """Block table and lengths of a cache that is kept in another form."""
+
+    def struct(self) -> KV:
+        raise LocksError("an 8-bit cache's view has its block table and lengths only: this call reads keys or values")
 
 
 class Context:
@@ -397,13 +409,13 @@ class Context:
                                                _stream(stream)), "locks_fake_quantize_pages")
 
     def locks_scan(self, q, summaries, kv: KVView, batch, head_logz, page_logmass=None, stream=None):
-        s = kv.struct()
+        s = kv.tables()
         _check(lib().locks_scan(self.handle, _ptr(q), _ptr(summaries), C.byref(s), batch, _ptr(page_logmass), _ptr(head_logz),
                                 _stream(stream)), "locks_scan")
 
     def locks_select_scored(self, head_logz_parts, kv: KVView, batch, page_ids, page_count, page_logshare=None,
                             page_logmass=None, stream=None):
-        s = kv.struct()
+        s = kv.tables()
         _check(lib().locks_select_scored(self.handle, _ptr(page_logmass), _ptr(head_logz_parts), int(head_logz_parts.shape[0]),
                                          C.byref(s), batch, _ptr(page_ids), _ptr(page_count), _ptr(page_logshare),
                                          _stream(stream)), "locks_select_scored")
@@ -418,7 +430,7 @@ class Context:
 
     def locks_select(self, q, summaries, kv: KVView, batch, page_ids, page_count, page_logmass=None,
                      page_logshare=None, stream=None):
-        s = kv.struct()
+        s = kv.tables()
         _check(lib().locks_select(self.handle, _ptr(q), _ptr(summaries), C.byref(s), batch, _ptr(page_ids),
                                   _ptr(page_count), _ptr(page_logmass), _ptr(page_logshare), _stream(stream)),
                "locks_select")
@@ -438,7 +450,7 @@ class Context:
 
     def locks_selection_quality(self, exact_logmass, kv: KVView, batch, page_ids, page_count, ref_ids, ref_count,
                                 quality, marked_pages=None, stream=None):
-        s = kv.struct()
+        s = kv.tables()
         n_marked = 0 if marked_pages is None else int(marked_pages.shape[-1])
         _check(lib().locks_selection_quality(self.handle, _ptr(exact_logmass), C.byref(s), batch, _ptr(page_ids),
                                              _ptr(page_count), _ptr(ref_ids), _ptr(ref_count), _ptr(marked_pages),

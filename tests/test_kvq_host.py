@@ -1,4 +1,6 @@
 """CPU: what the calls around a decode step refuse before anything reaches a GPU."""
+import inspect
+
 import pytest
 import torch
 
@@ -83,6 +85,27 @@ def test_library_refuses_bad_arguments_without_a_context():
     assert L.locks_kvq_append(None, None, None, None, 1, None, None, C.byref(rows), C.byref(rows), None, 1, None) == -1
     assert L.locks_kvq_attend(None, None, None, 1, None, 1, None, None, None, None, None) == -1
     assert L.locks_kvq_build_summaries(None, None, 1, None, None, None, None) == -1
+
+
+def test_the_view_for_the_selector_is_no_cache():
+    """Codes are one byte each: a call that took the view for rows of the configuration's type would read beyond them."""
+    view = cpu_view().kv_view()
+    assert view.tables().seq_lens == view.seq_lens.data_ptr() and view.tables().num_blocks == 4
+    with pytest.raises(locks.LocksError, match="reads keys"):
+        view.struct()
+    reads = ["locks_build_summaries", "locks_sparse_attend", "locks_decode_step", "locks_decode_step_host", "locks_select_exact", "locks_select_rival",
+             "locks_fake_quantize_pages", "locks_build_summaries_layers"]
+    ctx = object.__new__(locks.Context)
+    ctx.handle = None
+    for name in reads:
+        call = getattr(ctx, name)
+        args = {p: view if p == "kv" else ([torch.zeros(1)] if p.endswith("_layers") else None) for p in inspect.signature(call).parameters}
+        if "scorer" in args:
+            args["scorer"] = 1
+        with pytest.raises(locks.LocksError, match="reads keys"):
+            call(**args)
+    with pytest.raises(locks.LocksError, match="reads keys"):
+        locks.locks_sparse_attend_noalloc(binding.make_config(4, 2, 8, "i4", "bf16", 2, 4, 32), None, view, 2, None, None, None)
 
 
 def test_tails_of_one_or_two_pages():
