@@ -424,7 +424,8 @@ typedef struct {
 } locks_kvq;
 
 /* locks_append_rows for the 8-bit cache.  bf16 configurations (else UNSUPPORTED), pages of 16, 32 and 64 tokens.  cu_tokens has to
- * ascend; a request whose rows do not lie in 0 .. num_tokens is reported (LOCKS_ERR_BAD_BLOCK) and left out. */
+ * ascend; a request whose rows do not lie in 0 .. num_tokens is reported (LOCKS_ERR_BAD_BLOCK) and left out, and so are offsets that give
+ * rows to several requests where not all of their pages can be worked on. */
 int locks_kvq_append(locks_ctx *ctx, const locks_rotary *rot, const int32_t *positions, const int32_t *cu_tokens, int num_tokens,
                      const locks_rows *q, const locks_rows *q_out, const locks_rows *k_new, const locks_rows *v_new,
                      const locks_kvq *kv, int batch, locks_stream stream);

@@ -349,7 +349,7 @@ __global__ void __launch_bounds__(kQThreads, 2) kvq_append_kernel(const __grid_c
           set_status(a.status, LOCKS_ERR_BAD_BLOCK);
           m = 0;
         }
-        if (m > 0) items = max(1, T / B - (T - m) / B);
+        if (m > 0) items = max(1, T / B - (T - m) / B);   // (at most one more than p.n / B)
       }
       int sum = items;
 #pragma unroll
@@ -371,6 +371,7 @@ __global__ void __launch_bounds__(kQThreads, 2) kvq_append_kernel(const __grid_c
       __syncthreads();
       if (before > cta && cta + 1 < ctas) break;   // (the last CTA looks at every request)
     }
+    if (cta + 1 == ctas && before > ctas && tid == 0) set_status(a.status, LOCKS_ERR_BAD_BLOCK);   // offsets that go back: some items have no CTA
     if (found_s[0] < 0) return;
     b = found_s[0]; item = found_s[1]; row0 = found_s[2]; n = found_s[3];
   }

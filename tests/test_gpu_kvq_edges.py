@@ -272,3 +272,26 @@ def test_append_of_negative_lengths():
         assert ctx.locks_poll_status() == status
         used = [int(x) for x in (kvq.k_scale.abs().sum(1) > 0).nonzero()[:, 0]]
         assert used == [3] and not bool(kvq.k_tail[0].any())
+
+
+def test_append_offsets_that_go_back():
+    """Offsets that give all rows to every other request: more pages than there are CTAs for, which is reported; and one request's rows out of
+    range among others whose appends take place."""
+    n, B, batch, heads = 160, 16, 9, 2
+    k = torch.randn(n, heads, 128, generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).to(DEV)
+    table = torch.arange(batch * 12, dtype=torch.int32, device=DEV).view(batch, 12)
+    kvq = new_kvq_cache(batch * 12, batch, heads, B, table, torch.full((batch,), n, dtype=torch.int32, device=DEV))
+    ctx = context(4, heads, batch=batch, pages=12)
+    ctx.locks_kvq_append(k, k, kvq, batch, cu_tokens=torch.tensor([0 if b % 2 == 0 else n for b in range(batch + 1)], dtype=torch.int32, device=DEV))
+    assert ctx.locks_poll_status() == -6
+    for cu, good in (([0, 40, 90, 80, 160], [True, True, False, True]), ([0, 40, 170, 100, 160], [True, False, False, True])):
+        kvq = new_kvq_cache(48, 4, heads, B, table[:4].contiguous(), torch.tensor([100, 100, 100, 100], dtype=torch.int32, device=DEV))
+        ctx.locks_kvq_append(k, k, kvq, 4, cu_tokens=torch.tensor(cu, dtype=torch.int32, device=DEV))
+        assert ctx.locks_poll_status() == -6
+        assert [bool((kvq.k_scale.view(4, 12, heads)[b] > 0).any()) for b in range(4)] == good
+    # ragged offsets that are in order: as many pages as there can be, nothing reported
+    new = [17, 15, 31, 1, 33, 16, 15, 31, 1]
+    kvq = new_kvq_cache(batch * 12, batch, heads, B, table, torch.tensor([m + 15 for m in new], dtype=torch.int32, device=DEV))
+    ctx.locks_kvq_append(k, k, kvq, batch, cu_tokens=U.cu_of(new, DEV))
+    assert ctx.locks_poll_status() == 0
+    assert [int((kvq.k_scale.view(batch, 12, heads)[b, :, 0] > 0).sum()) for b in range(batch)] == [(m + 15) // 16 for m in new]
