@@ -111,7 +111,7 @@ typedef struct {
 size_t locks_summary_bytes(const locks_config *cfg);
 
 /* Bytes of device workspace locks_create() needs for this configuration (256-byte aligned
- * base).  0 on an invalid config. */
+ * base).  0 on an invalid config.  In bf16 configurations 19.6 MB of it are for attention over an 8-bit cache, whether there is one or not. */
 size_t locks_workspace_bytes(const locks_config *cfg);
 
 /* Validate the configuration, record it and the workspace pointer, zero the status word (one
@@ -444,9 +444,14 @@ int locks_kvq_append(locks_ctx *ctx, const locks_rotary *rot, const int32_t *pos
  * 0 .. num_tokens, or descending) are reported and left as they were, and so are all rows if such offsets give them to several requests
  * so often that there are more than batch + num_tokens tiles of them.  Partial results lie in the context's workspace: calls on one
  * context that overlap race on it, as locks_select's and locks_sparse_attend's do.
+ * Numbers: codes are exact, sums, maxima and log-sum-exp fp32.  Rounded to fp16 are a query's elements (each within 2^-25 of its row's largest,
+ * exact from 2^-17 of it on), the weights (2^-11 of each, in the few-row form down to 2^-29 of the largest, with the page's value scale in the many-row
+ * form) and the unfinished page's values (2^-11); its keys keep 22 bits.  Signed codes are multiplied as code + 128 in the few-row form, which leaves an error of
+ * 17 x 255 x 2^-23 of weight times scale.  Together they are below the rounding of the result to bf16 (1.65e-3 where fp32 arithmetic has 1.64e-3).
  * Where cu_tokens is given and rows are many (96 or more per KV head and request on average), queries times weights run on tcgen05
  * with weights relative to the largest value scale of the pages that a row sees: a page whose values are smaller than that by
- * more than 2^20 loses precision.  LOCKS_ERR_TOO_LARGE: more rows or pages than a launch can number (beyond 2^31 in all). */
+ * more than 2^20 loses precision.  The form is chosen for the call by that average: a prompt's chunk and single tokens are answered sooner
+ * by a call each (on slices of the tables, lengths and tails) than together.  LOCKS_ERR_TOO_LARGE: more rows or pages than a launch can number (beyond 2^31 in all). */
 int locks_kvq_attend(locks_ctx *ctx, const void *q, const int32_t *cu_tokens, int num_tokens, const locks_kvq *kv, int batch,
                      const int32_t *page_ids, const int32_t *page_count, void *out, float *lse, locks_stream stream);
 

@@ -18,9 +18,10 @@
 // problems, and a problem that several CTAs share is put together by the last of them, or by a second kernel where they are many.
 // A warp streams every fourth pair of a segment through a ring in shared memory and reads it as MMA fragments: the order of
 // dimensions in q k and of tokens and dimensions in p v is free, and is chosen such that a lane's bytes are 16-byte pieces of rows.
-// Measured, 32 query heads: 8 x 32K tokens over 8 KV heads 92 to 98 us (5.6 TB/s, 0.84 of a copy's bandwidth, which bounds it); one
-// request of 1M tokens over 2 KV heads 108 to 114 (0.74: the issue of conversions and products for 16 rows); 2048 listed tokens of 8
-// requests 21, of which 5 are bytes: the chain page id, block, scale, codes, and the join.
+// Measured, 32 query heads: 8 x 32K tokens over 8 KV heads 94 to 98 us (5.5 TB/s, 0.84 of a copy's bandwidth, which bounds it); one
+// request of 1M tokens over 2 KV heads 114 when the chip is busy all the time (0.72; 101 in short runs; signed codes 119: the issue of
+// conversions and products for 16 rows); 2048 listed tokens of 8 requests 21, of which 5 are bytes: the chain page id, block, scale,
+// codes, and the join (attention over the same pages of a 16-bit cache: 15 to 19 in one graph, so 8 bits save memory there, not time).
 #include <algorithm>
 
 #include "kvq.cuh"
@@ -914,8 +915,10 @@ extern "C" int locks_kvq_attend(locks_ctx *ctx, const void *q, const int32_t *cu
   p.c2 = ctx->cfg.sm_scale * kLog2e;
   // Chunks of prompts, from 96 query rows a KV head and request on average, and 768 in all (20 to 24 tokens of 32 heads): the form with 256
   // rows a CTA.  Measured either side, us, this form and that, 32 query heads: one request at 16301 with 8 KV heads 41 / 43 (16 tokens),
-  // 58 / 47 (32), 183 / 73 (128), 1361 / 362 (1024); six at 6000 113 / 58 (32 each); with 2 KV heads 38 / 32 (8 each); 24 at 3000 with 8 KV
-  // heads 132 / 138 (16 each), 246 / 138 (32).  Also where the line of this form may not fit 32 bits.
+  // 58 / 46 (32), 183 / 74 (128), 1361 / 374 (1024); six at 6000 113 / 60 (32 each); with 2 KV heads 38 / 32 (8 each); 24 at 3000 with 8 KV
+  // heads 132 / 138 (16 each), 246 / 139 (32).  Also where the line of this form may not fit 32 bits.  (The host knows the average alone: a
+  // batch of a chunk and single tokens takes one form for both, which costs up to 2.4 times what two calls do: 512 tokens beside 31 single ones at
+  // 8000 533 us, as two calls 221; 1024 beside 15 337 and 257; 2048 beside 24 at 16000 1205 and 823.)
   const int64_t problem = (((int64_t)(page_ids ? p.kbud : p.c.Pmax) << p.sub_shift) + 1) / 2 + kMostLead;   // places at most
   const bool fits = (batch + (cu_tokens ? (int64_t)num_tokens : 0)) * p.Hkv * problem <= INT32_MAX;
   if (cu_tokens && (!fits || ((int64_t)num_tokens * p.G >= (int64_t)96 * batch && (int64_t)num_tokens * p.Hq >= 768))) {

@@ -18,10 +18,10 @@
 // cores.  Why the scores are read once: a maximum that may be exceeded needs no second pass, and the next 32 columns' maximum hides
 // between these 32's exponentials.  Registers are split by warps' kind (setmaxnreg).  Where blocks of 256 rows are fewer than SMs, the
 // tokens that each sees are shared by several CTAs, and a second kernel joins them.
-// Measured, 1024 tokens of 32 heads over 8 KV heads after 15277: 369 us, 718 TFLOP/s, 0.43 of a library matrix product's rate (with 128 of 148
-// SMs at work: a CTA for each block); without the softmax 252, without products and conversion 276.  Pipes are about half busy
+// Measured, 1024 tokens of 32 heads over 8 KV heads after 15277: 374 us, 708 TFLOP/s, 0.42 of a library matrix product's rate (with 128 of 148
+// SMs at work: a CTA for each block); without the softmax 252, without products and conversion 276 (of 369 then).  Pipes are about half busy
 // (exponentials 50 %, tensor cores 40 %, issue 43 %): bound by the latencies of a chain of softmax and products with two softmax warps a
-// scheduler.  One request's tokens after 16K: 47 us (32 tokens), 73 (128), 205 (512).  Accumulators add up in the tensor cores' fp32.
+// scheduler.  One request's tokens after 16K: 46 us (32 tokens), 74 (128), 210 (512).  Accumulators add up in the tensor cores' fp32.
 #include <algorithm>
 #include <type_traits>
 
@@ -61,7 +61,7 @@ struct ChunkParams {
   __nv_bfloat16 *out;
   float *lse, *part, *part_lse;   // (partials of the splits: [block, head][split][2 x 128 rows], normalised, and log2 of their sums)
   int32_t *status;
-  int n, batch, Hq, G, tile_tokens, log_b, slots;   // slots: CTAs that may leave partials   // tile_tokens: of 128 rows
+  int n, batch, Hq, G, tile_tokens, log_b, slots;   // tile_tokens: of 128 rows; slots: CTAs that may leave partials
   float c2;
 };
 

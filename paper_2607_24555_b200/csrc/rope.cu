@@ -2,7 +2,8 @@
 //
 // A pair (a, b) of a head's dimensions turns by the angle position x frequency: (a cos - b sin, a sin + b cos).  Angles are formed in
 // fp64 turns (at position 10^6 the product's rounding to fp32 would be 0.03 rad), reduced to a fraction of a turn, and only then
-// go to fp32; rows are turned in fp32 and rounded once.  A token's cosines and sines are worked out once, in shared memory, for
+// go to fp32; rows are turned in fp32 and rounded once.  (An fp32 row is within 5.6e-8 of the exact one, relative, where sines and cosines in
+// fp64 would leave 4.2e-8; a bf16 row's rounding is 1.7e-3.)  A token's cosines and sines are worked out once, in shared memory, for
 // all of its heads.
 #include <algorithm>
 
@@ -112,8 +113,8 @@ struct RopeParams {
 // A CTA of NT threads takes one token row (ONE), or up to kRopeTokens: NT / 8 heads at a time, each by eight threads of which one has a
 // unit.  A thread fetches four units at a time, of four tokens (ONE: of four of its heads), while it turns the four before.  Bound by
 // the chain of a few round trips when there are few tokens (lengths and offsets; block; and rows, which are fetched meanwhile), by
-// memory when there are many.  8191 tokens of 32 + 8 heads are turned in 33 us (5.1 TB/s, 0.77 of a copy's bandwidth; 26 at all of it), 24 in
-// 3.3; 4K tokens appended in 24.7 (4.9 TB/s), 32 in 3.9.
+// memory when there are many.  8191 tokens of 32 + 8 heads are turned in 33 us (5.1 TB/s, 0.77 of a copy's bandwidth; 26 at all of it; fp32 72,
+// 51 at all of it), 24 in 3 to 4; 4K tokens appended in 24.8 (4.8 TB/s; fp32 55 of 37), 32 in 3.5 to 4.4.
 constexpr int kRopeThreads = 128, kRopeTokens = 16, kAhead = 4;
 
 struct RowsShared {
@@ -304,7 +305,7 @@ template <int FMT> __device__ __forceinline__ uint32_t code4(const float *v, flo
 // head's keys or values in registers (a lane: a unit of four tokens), so that the largest magnitude is known before a code is
 // written and everything is read once; pages of 32 and 64 tokens are two and four warps'
 // work.  The CTA's cosines and sines serve all heads.  Twelve prompts of 1.1K tokens on average with 32 heads of queries: 73 us (4.3 TB/s; 48 at a
-// copy's bandwidth); 8 single tokens 6.3.
+// copy's bandwidth), signed codes 75, in pages of 32 and 64 tokens 82 and 99 (fewer CTAs, and a head's turn after the other); 8 single tokens 6.3 to 6.9.
 // EARLY (where offsets are given, so that pages get many tokens): the first round's rows are fetched before the cosines are worked out (12
 // prompts together: 82 to 73 us; one token per request, where it would wait for nothing, 6.3 to 6.9 from the registers that it costs).
 template <int FMT, bool EARLY>
