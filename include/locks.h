@@ -398,7 +398,7 @@ int locks_append_rows(locks_ctx *ctx, const locks_rotary *rot, const int32_t *po
  *   LOCKS_KVQ_INT    signed integers: scale = max |x| / 127, code = x / scale rounded to even
  *   LOCKS_KVQ_FLOAT  four exponent and three fraction bits (e4m3): scale = max |x| / 448, code = x / scale rounded to even
  * A page whose largest magnitude is below 2^-100 is stored as zeros with a scale of zero; one with an infinity or a NaN gets a
- * scale of NaN and codes of zero: whatever attends it is NaN.  Scales are fp32.
+ * scale of NaN and codes of zero: whatever attends it is NaN.  Scales are fp32, not negative.
  * Only complete pages are in codes.  The unfinished last page of the request in row b of the batch is kept as it comes, in fp32, in
  * k_tail / v_tail [max_batch][Hkv][tail_pages * page_size][head_dim] (page p in the tail's page p % tail_pages), and is quantised once,
  * when its last token comes; so the codes do not depend on how a sequence was cut into appends.  A request that moves to
@@ -408,8 +408,9 @@ int locks_append_rows(locks_ctx *ctx, const locks_rotary *rot, const int32_t *po
  *   tail_pages 1   to M / page_size * page_size: not into a page that has been completed.  For that, keep a copy of the row's tails from before
  *                  the append that completed it, put it back, and append the tokens that stay once more;
  *   tail_pages 2   to (M / page_size - 1) * page_size: into the last page that has been completed, too.
- * Below that the rows are gone, which nothing can see: no status is set.  A page's codes are written anew when it is completed anew (and a
- * summary of it is the caller's to build again). */
+ * Below that, or in a page that no append of this row's completed (a shared prefix), the rows are not there, which nothing can see: no status
+ * is set.  A page's codes are written anew when it is completed anew, so no other request may share its block by then, and a summary of it is
+ * the caller's to build again. */
 #define LOCKS_KVQ_INT 0
 #define LOCKS_KVQ_FLOAT 1
 typedef struct {
@@ -444,7 +445,7 @@ int locks_kvq_append(locks_ctx *ctx, const locks_rotary *rot, const int32_t *pos
  * 0 .. num_tokens, or descending) are reported and left as they were, and so are all rows if such offsets give them to several requests
  * so often that there are more than batch + num_tokens tiles of them.  Partial results lie in the context's workspace: calls on one
  * context that overlap race on it, as locks_select's and locks_sparse_attend's do.
- * Numbers: codes are exact, sums, maxima and log-sum-exp fp32.  Rounded to fp16 are a query's elements (each within 2^-25 of its row's largest,
+ * Numbers: queries below 2^100 in magnitude; codes are exact, sums, maxima and log-sum-exp fp32.  Rounded to fp16 are a query's elements (each within 2^-25 of its row's largest,
  * exact from 2^-17 of it on), the weights (2^-11 of each, in the few-row form down to 2^-29 of the largest, with the page's value scale in the many-row
  * form) and the unfinished page's values (2^-11); its keys keep 22 bits.  Signed codes are multiplied as code + 128 in the few-row form, which leaves an error of
  * 17 x 255 x 2^-23 of weight times scale.  Together they are below the rounding of the result to bf16 (1.65e-3 where fp32 arithmetic has 1.64e-3).

@@ -160,6 +160,28 @@ def test_captured_drafts(m):
     torch.cuda.current_stream().wait_stream(side)
 
 
+@pytest.mark.parametrize("B", [16, 32, 64])
+@pytest.mark.parametrize("lens", [[150, 203], [128 + 31, 64 + 17], [192, 255]])
+def test_chunks_find_the_tail(lens, B):
+    """The many-row form, unfinished pages in either page of the tail; an infinite value in one of them."""
+    gen = torch.Generator().manual_seed(B)
+    k, v = [[rows(gen, t, Hkv, "bf16") for t in lens] for _ in range(2)]
+    a, c = Cache(B, 2, 20, "int8", tail_pages=2), Cache(B, 2, 20, "int8")
+    before, new = [t // 3 for t in lens], [min(t, 100) for t in lens]
+    for o in (a, c):
+        o.append(k, v, before, before)
+        o.append(k, v, lens, [t - n for t, n in zip(lens, before)])
+    q = rows(gen, sum(new), Hq, "bf16")
+    assert sum(new) * 4 >= 96 * 2 and sum(new) * Hq >= 768
+    for turn in range(2):
+        got = [o.attend(q, lens, new) for o in (a, c)]
+        for x, y in zip(*got):
+            assert torch.equal(x, y) and not bool(torch.isnan(x.float()).any())
+        assert bool(torch.isfinite(got[0][0].float()).all()) == (turn == 0 or lens[0] % B == 0)
+        for o in (a, c):
+            o.kvq.v_tail[0, 1, lens[0] // B % o.kvq.tail_pages * B, 5] = float("inf")
+
+
 def test_tails_of_other_sizes_are_refused():
     a = Cache(16, 1, 4, "int8")
     s = a.kvq.struct()
