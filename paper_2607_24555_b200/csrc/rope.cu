@@ -487,7 +487,8 @@ __global__ void __launch_bounds__(kQThreads, 2) kvq_append_kernel(const __grid_c
           if (lane == 0 && sub == 0) (key ? c.ks : c.vs)[(int64_t)block * c.Hkv + h] = scale;
         }
       }
-      // (a page that is complete keeps its rows where the tail has two pages, so that the sequence may be shortened into it)
+      // (a page that is complete keeps its rows where the tail has two pages, so that the sequence may be shortened into it: 12 prompts
+      // 72.7 us with one page, 78.4 with two, single tokens 6.4 and 6.6)
       if (live && fits && (!complete || (c.tail_pages == 2 && page == p0 && page == last - 1))) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
